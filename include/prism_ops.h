@@ -160,6 +160,102 @@ PRISM_API int prism_op_route_static(const float* scores, const int32_t* cu_old, 
 PRISM_API int prism_op_compact(const float* x_old, float* x_new, const int32_t* cu_old, const int32_t* cu_new,
                      const int32_t* old_of_new, int32_t n_new, int32_t total_new, int32_t d, void* stream);
 
+/* ---- paged key/value cache -----------------------------------------------------------------------------------
+ * Keys and values that outlive a call: a prompt that many candidates read, a document fed in chunks, one more token
+ * per candidate.  (The paper recomputes every sequence in every request and has no counterpart.)  They lie in pages of
+ * page_size tokens; row s of the block table names the pages of sequence s in order, and token t of the sequence lies in
+ * SLOT table[s][t / page_size] * page_size + t % page_size.  Within page p, head h holds page_size consecutive rows of
+ * head_dim elements: element ((p * page_stride) + (h * page_size + row) * head_dim) of k and of v.
+ *
+ * One step of a model:  prism_op_page_append (pages, positions and slots of the new tokens), prism_op_attention_paged_plan,
+ * then per layer prism_op_qknorm_rope_paged (new keys and values into that layer's cache) and prism_op_attention_paged;
+ * prism_op_page_release when a probe has dropped candidates (old_of_new of prism_op_route names the survivors).
+ *
+ * Limits: page_size 16, 32, 64, 128 or 256; n_seq <= PRISM_MAX_CANDIDATES; (pages + 1) * page_size below 2^31, for the
+ * cache and for a block-table row; head_dim a multiple of 16, at most 256; pointers to matrices, plan and workspace 16-byte
+ * aligned, strides (in ELEMENTS) multiples of 16 bytes.  err_word (device int32, zeroed by the caller, bits stay set):
+ *   2   bad lengths, offsets or survivors, or a plan made for another shape      4   an expired bounded wait
+ *   16  a page id or slot outside the cache, or a sequence longer than its block-table row
+ *   32  not enough free pages (append), or no room in the pool (release)
+ * No entry point allocates, copies to the host or synchronises; all of them may be captured into a graph.  Calls that run at
+ * the same time need workspaces of their own; a plan may be shared by them. */
+typedef struct {
+  void* k;              /* device */
+  void* v;              /* device */
+  int64_t page_stride;  /* elements from one page to the next, the same for k and v */
+  int32_t num_pages, page_size, n_kv_heads, head_dim;
+  int32_t dtype;        /* PRISM_FP32 or PRISM_BF16 */
+} prism_kv_cache;
+
+/* Pages and slots for len_new[s] >= 0 new tokens of every sequence, which holds kv_len_in[s] tokens already:
+ *   kv_len_out[s] = kv_len_in[s] + len_new[s];  cu_q[n_seq+1] = exclusive scan of len_new;
+ *   for row cu_q[s] + i:  pos = kv_len_in[s] + i,  slot_map = that token's slot;
+ *   rows cu_q[n_seq] .. total (padding of a fixed-size step): pos 0, slot -1.
+ * A sequence needs ceil(kv_len_out / page_size) pages; the missing ones are taken off the stack free_pages[num_pages] (which
+ * keeps its contents), in order of sequence, then position: the k-th new page is free_pages[*n_free_in - 1 - k].  They are
+ * entered into block_table[n_seq][max_pages] (rows table_stride apart; other entries stay), and *n_free_out is what is left.
+ * kv_len_out may be kv_len_in and n_free_out may be n_free_in.  Refused as a whole, with an error bit: a negative length, a
+ * sequence beyond max_pages, more rows than `total`, too few free pages; then kv_len_out = kv_len_in, *n_free_out =
+ * *n_free_in, cu_q = 0, every slot -1 and the table is untouched.  A page id outside [0, num_pages) sets bit 16, is
+ * entered as -1 and its rows get slot -1. */
+PRISM_API int prism_op_page_append(const int32_t* len_new, const int32_t* kv_len_in, int32_t* kv_len_out, int32_t n_seq,
+                                   int32_t page_size, int32_t num_pages, int32_t max_pages, int64_t table_stride,
+                                   int32_t* block_table, const int32_t* free_pages, const int32_t* n_free_in, int32_t* n_free_out,
+                                   int32_t total, int32_t* cu_q, int32_t* pos, int32_t* slot_map, int32_t* err_word, void* stream);
+
+/* The counterpart of prism_op_compact: new sequence i < n_new is old sequence old_of_new[i] (distinct, any order); the
+ * other sequences leave and their pages, except the first shared_pages entries of every row (a prefix that other sequences
+ * read), go on top of the free stack in order of sequence, then position.  Writes all n_seq rows of table_out (must not
+ * overlap table_in) and kv_len_out (may be kv_len_in): entries behind a row's last page and rows behind the last
+ * survivor become -1, their lengths 0.  Refused as a whole, with an error bit: a survivor outside [0, n_seq) or named
+ * twice, a length outside [0, max_pages * page_size], a stack that would exceed num_pages; then lengths, table, stack and
+ * counter come out as they went in. */
+PRISM_API int prism_op_page_release(const int32_t* old_of_new, int32_t n_new, const int32_t* kv_len_in, int32_t* kv_len_out,
+                                    int32_t n_seq, int32_t page_size, int32_t num_pages, int32_t shared_pages, int32_t max_pages,
+                                    int64_t stride_in, const int32_t* table_in, int64_t stride_out, int32_t* table_out,
+                                    int32_t* free_pages, const int32_t* n_free_in, int32_t* n_free_out, int32_t* err_word,
+                                    void* stream);
+
+/* prism_op_qknorm_rope into the cache, one pass: for every row of qkv [rows, (Hq+2Hkv)*head_dim] (rows qkv_stride apart)
+ * the optional per-head RMSNorm and the rotary embedding of the q and k heads at position pos[row]; q goes to
+ * q_out [rows, Hq*head_dim] (rows q_stride apart; may be the q columns of qkv itself, with the same stride), k and v to slot
+ * slot_map[row] of the cache.  Angles are taken in 64 bits, so positions have no limit and no table.  A row with a
+ * negative slot is padding: nothing is written for it; a slot beyond the cache sets bit 16 and writes nothing either.
+ * Slots >= 0 of one call must be distinct. */
+PRISM_API int prism_op_qknorm_rope_paged(const void* qkv, int64_t qkv_stride, const int32_t* pos, const int32_t* slot_map,
+                                         int32_t rows, int32_t n_q_heads, int32_t qk_norm, const void* g_q, const void* g_k,
+                                         float eps, float theta, void* q_out, int64_t q_stride, const prism_kv_cache* cache,
+                                         int32_t* err_word, void* stream);
+
+/* Attention of every sequence's new tokens over its cached and new keys.  Row cu_q[s] + i of q [total_q, Hq*head_dim] is
+ * the token at position kv_len[s] - (cu_q[s+1] - cu_q[s]) + i; query head h reads key/value head h / (Hq/Hkv):
+ *   out = softmax(q k^T / sqrt(head_dim)) v over the keys at positions <= its own (causal) or < kv_len[s].
+ * A row that sees no key gets zeros; rows outside cu_q[0] .. cu_q[n_seq] are left as they were.  Slots behind
+ * kv_len[s] may hold anything; a value of a key that SOME row of the same sequence sees must be finite, or it may reach rows
+ * of that sequence's call that do not see it.
+ *
+ * The lengths stay on the device, so the work is laid out there, once a step, for all layers of a model:
+ * prism_op_attention_paged_plan reads cu_q and kv_len and writes the plan; prism_op_attention_paged then takes the same
+ * n_seq, total_q (rows of q), max_q_len (no sequence has more new rows), heads, dtype and impl.
+ * prism_op_attention_paged_bytes (host only) gives the sizes of plan and workspace; the workspace is scratch of one call
+ * and may be NULL when max_pages * page_size <= 256.
+ * impl: PRISM_IMPL_AUTO = tensor cores for bf16 at head_dim 64 and 128 (Hq/Hkv <= 128): warp-level MMA with the cache streamed
+ * through shared memory when max_q_len * Hq/Hkv <= 16, else tcgen05; CUDA cores otherwise (Hq/Hkv <= 64).
+ * PRISM_IMPL_SIMT = CUDA cores.  Results do not depend on other sequences' contents; they may differ in rounding between plans
+ * that cut a sequence differently. */
+PRISM_API int prism_op_attention_paged_bytes(int32_t n_seq, int32_t total_q, int32_t max_q_len, int32_t n_q_heads,
+                                             int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t impl,
+                                             int64_t* plan_bytes, int64_t* workspace_bytes);
+PRISM_API int prism_op_attention_paged_plan(const int32_t* cu_q, const int32_t* kv_len, int32_t n_seq, int32_t total_q,
+                                            int32_t max_q_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                            int32_t dtype, int32_t causal, int32_t impl, void* plan, int64_t plan_bytes,
+                                            int32_t* err_word, void* stream);
+PRISM_API int prism_op_attention_paged(const void* q, int64_t q_stride, const prism_kv_cache* cache, const int32_t* block_table,
+                                       int64_t table_stride, int32_t max_pages, const void* plan, int64_t plan_bytes, int32_t n_seq,
+                                       int32_t total_q, int32_t max_q_len, int32_t n_q_heads, int32_t impl, void* out,
+                                       int64_t out_stride, void* workspace, int64_t workspace_bytes, int32_t* err_word,
+                                       void* stream);
+
 /* Self-test of the bounded device-side wait that every tensor-core kernel uses (PRISM_ERR_TIMEOUT path):
  * one thread waits on a barrier that nothing arrives at, gives up after limit_cycles (1 .. 2e9 SM clock
  * cycles), sets bit 4 of err_word (device int32, zeroed by the caller) and the kernel returns.  Nothing

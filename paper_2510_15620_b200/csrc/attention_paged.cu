@@ -1,0 +1,464 @@
+// Attention over a paged cache: the work list, the CUDA-core kernel, and the pass that joins partial results.
+//
+// For token t of sequence s, at position p = kv_len[s] - new[s] + t, and query head h (key/value head h / group):
+//   out = sum_k softmax_k(q . K_k / sqrt(dh)) V_k   over keys k <= p (causal) or k < kv_len[s],
+// zero where no key is visible.  Softmax statistics and sums are fp32 throughout.
+#include <math.h>
+
+#include "paged.cuh"
+
+namespace prism {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+// ------------------------------------------------------------------------------------------------ work list
+// One block.  Tiles of s.tokens tokens; a tile whose keys are more than `piece` is cut into equal pieces so that few long
+// sequences still occupy every SM.  The piece length is the launch's total (keys x heads) over s.target, hence the bounds
+// of paged_plan_bounds.  Tiles are listed from the last to the first: under causal attention a sequence's last tile has the
+// most keys, and the launch should end on light ones.
+struct Sums {
+  long long a, b, c;
+};
+__device__ __forceinline__ Sums plan_scan(Sums v, Sums* warp_tot, Sums& tot) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  Sums inc = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long a = __shfl_up_sync(0xffffffffu, inc.a, d), b = __shfl_up_sync(0xffffffffu, inc.b, d),
+                    c = __shfl_up_sync(0xffffffffu, inc.c, d);
+    if (lane >= d) inc.a += a, inc.b += b, inc.c += c;
+  }
+  __syncthreads();  // the previous call's totals have been read
+  if (lane == 31) warp_tot[warp] = inc;
+  __syncthreads();
+  if (warp == 0) {
+    const Sums w = warp_tot[lane];
+    Sums wi = w;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long a = __shfl_up_sync(0xffffffffu, wi.a, d), b = __shfl_up_sync(0xffffffffu, wi.b, d),
+                      c = __shfl_up_sync(0xffffffffu, wi.c, d);
+      if (lane >= d) wi.a += a, wi.b += b, wi.c += c;
+    }
+    warp_tot[lane] = Sums{wi.a - w.a, wi.b - w.b, wi.c - w.c};
+    if (lane == 31) warp_tot[32] = wi;
+  }
+  __syncthreads();
+  tot = warp_tot[32];
+  const Sums e = warp_tot[warp];
+  return Sums{e.a + inc.a - v.a, e.b + inc.b - v.b, e.c + inc.c - v.c};
+}
+
+__global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restrict__ cu, const int* __restrict__ kv_len, int n,
+                                                             int total_q, int max_q, int hq, int hkv, int dh, int causal,
+                                                             PagedPlanShape sh, PagedPlanBounds bound, void* plan, int* err) {
+  extern __shared__ int s_tile[];  // [n + 1] first tile of each sequence
+  __shared__ Sums warp_tot[33];
+  const int tid = threadIdx.x;
+  PagedPlanHeader* hd = static_cast<PagedPlanHeader*>(plan);
+  PagedItem* items = reinterpret_cast<PagedItem*>(hd + 1);
+  PagedJoin* joins = reinterpret_cast<PagedJoin*>(items + bound.items);
+  const int per = (n + kPlanThreads - 1) / kPlanThreads, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  Sums mine{0, 0, 0}, tot;
+  bool bad = false;
+  for (int i = i0; i < i1; ++i) {
+    const int a = cu[i], b = cu[i + 1];
+    if (a < 0 || b < a || b > total_q || b - a > max_q || kv_len[i] < 0) bad = true;
+    else mine.a += (b - a + sh.tokens - 1) / sh.tokens;
+  }
+  Sums at = plan_scan(mine, warp_tot, tot);
+  bad = __syncthreads_or(bad);
+  for (int i = i0; !bad && i < i1; ++i) {
+    s_tile[i] = (int)at.a;
+    at.a += (cu[i + 1] - cu[i] + sh.tokens - 1) / sh.tokens;
+  }
+  const int n_tiles = bad ? 0 : (int)tot.a;
+  if (tid == 0) s_tile[n] = n_tiles;
+  __syncthreads();
+  struct Tile {
+    int seq, row0, n_tok, pos0, keys;
+  };
+  auto tile_at = [&](int t) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (s_tile[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    Tile r;
+    r.seq = lo;
+    const int a = cu[lo], q = cu[lo + 1] - a, first = (t - s_tile[lo]) * sh.tokens, kv = kv_len[lo];
+    r.row0 = a + first;
+    r.n_tok = min(sh.tokens, q - first);
+    r.pos0 = kv - q + first;
+    r.keys = causal ? max(0, r.pos0 + r.n_tok) : kv;
+    return r;
+  };
+  Sums w{0, 0, 0};
+  for (int t = tid; t < n_tiles; t += kPlanThreads) w.a += tile_at(t).keys;
+  plan_scan(w, warp_tot, tot);
+  long long piece = (tot.a * hkv + sh.target - 1) / sh.target;
+  piece = piece < sh.min_piece ? sh.min_piece : piece;
+  int base = 0, base_part = 0, base_join = 0;
+  for (int t0 = 0; t0 < n_tiles; t0 += kPlanThreads) {
+    const int i = t0 + tid, t = n_tiles - 1 - i;
+    Tile r{};
+    Sums c{0, 0, 0};
+    int len = 0;
+    if (t >= 0) {
+      r = tile_at(t);
+      const long long cuts = (r.keys + piece - 1) / piece;
+      if (cuts > 1) {
+        len = (int)(((r.keys + cuts - 1) / cuts + sh.piece_unit - 1) / sh.piece_unit * sh.piece_unit);
+        c.a = (r.keys + len - 1) / len;
+      } else {
+        c.a = 1;
+      }
+      if (c.a > 1) c.b = c.a, c.c = 1;
+    }
+    const Sums off = plan_scan(c, warp_tot, tot);
+    if (t >= 0) {
+      const int it = base + (int)off.a, part = base_part + (int)off.b;
+      for (int j = 0; j < (int)c.a; ++j) {
+        PagedItem x;
+        x.seq = r.seq, x.row0 = r.row0, x.n_tok = r.n_tok, x.pos0 = r.pos0;
+        x.k0 = c.a > 1 ? j * len : 0;
+        x.k1 = c.a > 1 ? (int)min((long long)r.keys, (j + 1ll) * len) : r.keys;
+        x.part = c.a > 1 ? part + j : -1;
+        x.pad = 0;
+        items[it + j] = x;
+      }
+      if (c.a > 1) {
+        PagedJoin x;
+        x.row0 = r.row0, x.n_tok = r.n_tok, x.pos0 = r.pos0, x.part0 = part, x.n_parts = (int)c.a, x.piece = len;
+        x.causal = causal, x.pad = 0;
+        joins[base_join + (int)off.c] = x;
+      }
+    }
+    base += (int)tot.a, base_part += (int)tot.b, base_join += (int)tot.c;
+  }
+  if (tid == 0) {
+    PagedPlanHeader x{};
+    x.kind = sh.kind, x.n_items = base, x.n_joins = base_join, x.causal = causal;
+    x.hq = hq, x.hkv = hkv, x.dh = dh, x.total_q = total_q, x.n_seq = n, x.max_q = max_q, x.rows = sh.rows;
+    *hd = x;
+    if (bad) atomicOr(err, kErrBadOffsets);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ joining pieces
+// out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i, M = max_i m_i, over the pieces in which the row sees a key.
+// Eight lanes share a (row, 16 columns): each takes every eighth piece, and a butterfly adds them in a fixed order.
+template <typename T>
+__global__ void __launch_bounds__(256) k_paged_join(PagedPlanHeader want, const PagedPlanHeader* __restrict__ hd,
+                                                    long long items_cap, const float* __restrict__ ws, T* __restrict__ out,
+                                                    long long out_stride) {
+  pdl_sync();
+  if (hd->kind != want.kind || hd->hq != want.hq || hd->hkv != want.hkv || hd->dh != want.dh || hd->total_q != want.total_q ||
+      hd->n_seq != want.n_seq || hd->max_q != want.max_q)
+    return;  // the attention kernel has reported it
+  const PagedJoin* joins = reinterpret_cast<const PagedJoin*>(reinterpret_cast<const PagedItem*>(hd + 1) + items_cap);
+  const int rows = want.rows, dh = want.dh, hkv = want.hkv, group = want.hq / hkv, chunks = dh / 16;
+  const long long per_join = (long long)hkv * chunks * rows, total = per_join * hd->n_joins;
+  const long long part_floats = paged_part_floats(rows, dh);
+  const int sub = threadIdx.x & 7;
+  for (long long u = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 3; u < total;
+       u += ((long long)gridDim.x * blockDim.x) >> 3) {
+    const PagedJoin jn = joins[u / per_join];
+    const int rem = (int)(u % per_join), r = rem % rows, ch = rem / rows % chunks, h = rem / rows / chunks;
+    const int tok = r / group;
+    if (tok >= jn.n_tok) continue;  // the eight lanes of a row agree
+    const unsigned lanes = 0xffu << (threadIdx.x & 24);
+    const int pos = jn.pos0 + tok;
+    // pieces in which this row sees a key
+    int n_parts = jn.n_parts;
+    if (jn.causal) n_parts = pos < 0 ? 0 : min(n_parts, pos / jn.piece + 1);
+    const float* base = ws + ((long long)jn.part0 * hkv + h) * part_floats;
+    const long long step = (long long)hkv * part_floats;
+    float m = -INFINITY;
+    for (int i = sub; i < n_parts; i += 8) m = fmaxf(m, base[i * step + (long long)rows * dh + 2 * r]);
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, d));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = 0.f;
+    for (int i = sub; i < n_parts; i += 8) {
+      const float* p = base + i * step;
+      const float2 ml = *reinterpret_cast<const float2*>(p + (long long)rows * dh + 2 * r);
+      const float w = exp2f(ml.x - ref);
+      l += w * ml.y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float4 v = *reinterpret_cast<const float4*>(p + ((long long)(ch * 4 + e) * rows + r) * 4);
+        o[4 * e] += w * v.x, o[4 * e + 1] += w * v.y, o[4 * e + 2] += w * v.z, o[4 * e + 3] += w * v.w;
+      }
+    }
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) {
+      l += __shfl_xor_sync(lanes, l, d);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e] += __shfl_xor_sync(lanes, o[e], d);
+    }
+    const float inv = n_parts > 0 ? 1.f / l : 0.f;
+    T* dst = out + (jn.row0 + tok) * out_stride + (long long)(h * group + r % group) * dh + ch * 16 + sub * 2;
+    float v0 = 0.f, v1 = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e == sub) v0 = o[2 * e], v1 = o[2 * e + 1];
+    v0 = n_parts > 0 ? v0 * inv : 0.f;
+    v1 = n_parts > 0 ? v1 * inv : 0.f;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(v0, v1);
+    else
+      *reinterpret_cast<float2*>(dst) = make_float2(v0, v1);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ CUDA-core kernel
+// fp32 (and bf16 at head sizes without a tensor-core kernel): R query rows against 64 keys at a time, 256 threads as a
+// 16 x 16 grid, each thread R/16 rows x 4 keys of the scores and R/16 rows x dh/16 columns of the output.  Keys and values
+// are widened to fp32 in shared memory; rows are padded by four floats so that the 16-byte reads of eight
+// neighbouring key rows fall into different banks.
+constexpr int kKeys = 64;
+
+__device__ __forceinline__ void store(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                     __uint_as_float(u.y & 0xffff0000u));
+}
+
+__host__ __device__ constexpr int simt_smem(int rows, int dh) {
+  return 4 * ((rows + 2 * kKeys) * (dh + 4) + rows * (kKeys + 4));
+}
+
+template <typename T, int R, int COLS>
+__global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, float scale_log2) {
+  pdl_sync();
+  extern __shared__ __align__(16) float sm[];
+  constexpr int RT = R / 16;
+  const PagedPlanHeader* hd = static_cast<const PagedPlanHeader*>(a.plan);
+  const int hkv = a.c.hkv, dh = a.c.dh, group = a.hq / hkv, ld = dh + 4;
+  if (hd->kind != kPagedSimt || hd->hq != a.hq || hd->hkv != hkv || hd->dh != dh || hd->total_q != a.total_q ||
+      hd->n_seq != a.n_seq || hd->max_q != a.max_q || hd->rows != R) {
+    if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(a.err, kErrBadOffsets);
+    return;
+  }
+  if (threadIdx.x == 0 && blockIdx.x == 0 && hd->n_items * hkv > (int)gridDim.x) atomicOr(a.err, kErrBadPage);
+  const int item = blockIdx.x / hkv, h = blockIdx.x % hkv;
+  if (item >= hd->n_items) return;
+  const PagedItem it = paged_item(hd, item, a.max_pages, shift, a.ws, a.err);
+  const int causal = hd->causal;
+  float* s_q = sm;
+  float* s_k = s_q + R * ld;
+  float* s_v = s_k + kKeys * ld;
+  float* s_p = s_v + kKeys * ld;
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, q4 = dh >> 2;
+  const T* q = static_cast<const T*>(a.q);
+  for (int u = tid; u < R * q4; u += 256) {
+    const int r = u / q4, c = (u % q4) * 4, tok = r / group;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (tok < it.n_tok) v = load4(q + (it.row0 + tok) * a.q_stride + (long long)(h * group + r % group) * dh + c);
+    *reinterpret_cast<float4*>(s_q + r * ld + c) = v;
+  }
+  // rows of this thread: ty + 16 i.  lim: keys below it are visible
+  int lim[RT];
+  float m[RT], l[RT], o[RT][COLS];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    const int r = ty + 16 * i, tok = r / group;
+    lim[i] = tok < it.n_tok ? (causal ? min(it.k1, it.pos0 + tok + 1) : it.k1) : 0;
+    m[i] = -INFINITY, l[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) o[i][c] = 0.f;
+  }
+  const int* row = a.table + it.seq * a.table_stride;
+  for (int k0 = it.k0; k0 < it.k1; k0 += kKeys) {
+    __syncthreads();
+    for (int u = tid; u < kKeys * q4; u += 256) {
+      const int kk = u / q4, c = (u % q4) * 4, key = k0 + kk;
+      float4 kf = make_float4(0.f, 0.f, 0.f, 0.f), vf = kf;
+      if (key < it.k1) {
+        const int j = key >> shift, id = j < a.max_pages ? row[j] : -1;
+        if ((unsigned)id < (unsigned)a.c.num_pages) {
+          const long long at = id * a.c.page_stride + (((long long)h << shift) + (key & ((1 << shift) - 1))) * dh + c;
+          kf = load4(static_cast<const T*>(a.c.k) + at);
+          vf = load4(static_cast<const T*>(a.c.v) + at);
+        } else if (c == 0) {
+          atomicOr(a.err, kErrBadPage);
+        }
+      }
+      *reinterpret_cast<float4*>(s_k + kk * ld + c) = kf;
+      *reinterpret_cast<float4*>(s_v + kk * ld + c) = vf;
+    }
+    __syncthreads();
+    float s[RT][4];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < dh; c += 4) {
+      float4 qa[RT], kb[4];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) qa[i] = *reinterpret_cast<const float4*>(s_q + (ty + 16 * i) * ld + c);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kb[j] = *reinterpret_cast<const float4*>(s_k + (tx + 16 * j) * ld + c);
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          s[i][j] += qa[i].x * kb[j].x + qa[i].y * kb[j].y + qa[i].z * kb[j].z + qa[i].w * kb[j].w;
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[i][j] = k0 + tx + 16 * j < lim[i] ? s[i][j] * scale_log2 : -INFINITY;
+        mx = fmaxf(mx, s[i][j]);
+      }
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+      const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.f : mn;
+      const float f = exp2f(m[i] - ref);
+      m[i] = mn;
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = exp2f(s[i][j] - ref);
+        sum += p;
+        s_p[(ty + 16 * i) * (kKeys + 4) + tx + 16 * j] = p;
+      }
+      l[i] = l[i] * f + sum;
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) o[i][c] *= f;
+    }
+    __syncwarp();  // a row's sixteen threads are half a warp
+    const int nk = min(kKeys, it.k1 - k0);
+    for (int kk = 0; kk < nk; ++kk) {
+      float p[RT];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) p[i] = s_p[(ty + 16 * i) * (kKeys + 4) + kk];
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) {
+        const float v = tx + 16 * c < dh ? s_v[kk * ld + tx + 16 * c] : 0.f;
+#pragma unroll
+        for (int i = 0; i < RT; ++i) o[i][c] += p[i] * v;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+    const int r = ty + 16 * i, tok = r / group;
+    if (tok >= it.n_tok) continue;
+    if (it.part < 0) {
+      const bool any = lim[i] > it.k0;
+      const float inv = 1.f / l[i];
+      T* dst = static_cast<T*>(a.out) + (it.row0 + tok) * a.out_stride + (long long)(h * group + r % group) * dh;
+#pragma unroll
+      for (int c = 0; c < COLS; ++c)
+        if (tx + 16 * c < dh) store(dst + tx + 16 * c, any ? o[i][c] * inv : 0.f);
+    } else {
+      float* p = a.ws + ((long long)it.part * hkv + h) * paged_part_floats(R, dh);
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) {
+        const int col = tx + 16 * c;
+        if (col < dh) p[((long long)(col >> 2) * R + r) * 4 + (col & 3)] = o[i][c];
+      }
+      if (tx == 0) *reinterpret_cast<float2*>(p + (long long)R * dh + 2 * r) = make_float2(m[i], l[i]);
+    }
+  }
+}
+
+int log2_of(int x) {
+  int s = 0;
+  while ((1 << s) < x) ++s;
+  return s;
+}
+
+template <typename T, int R, int COLS>
+cudaError_t simt_launch(const PagedAttnArgs& a, int grid, cudaStream_t st) {
+  static std::atomic<unsigned long long> set;
+  const int smem = simt_smem(R, a.c.dh);
+  if (cudaError_t e = ensure_dynamic_smem(k_paged_simt<T, R, COLS>, simt_smem(R, 16 * COLS), set)) return e;
+  const float scale_log2 = 1.4426950408889634f / sqrtf((float)a.c.dh);
+  k_paged_simt<T, R, COLS><<<grid, 256, smem, st>>>(a, log2_of(a.c.page_size), scale_log2);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool paged_plan_shape(int max_q, int hq, int hkv, int dh, int dtype, int impl, PagedPlanShape* s) {
+  const int g = hq / hkv;
+  if (max_q < 1) max_q = 1;
+  s->group = g;
+  s->piece_unit = 128;
+  const bool few = (long long)max_q * g <= 16;
+  if (dtype == 1 && impl == 0 && (dh == 64 || dh == 128) && g <= 128) {
+    if (few) {
+      // tokens: the whole sequence's new rows fit one 16-row tile
+      s->kind = kPagedTokens, s->rows = 16, s->tokens = 16 / g, s->min_piece = 256, s->target = 148 * 4;
+    } else {
+      s->kind = kPagedTiles, s->rows = 256, s->tokens = 2 * (128 / g), s->min_piece = 1024, s->target = 148 * 4;
+    }
+    return true;
+  }
+  if (g > 64) return false;
+  s->kind = kPagedSimt, s->rows = few ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 256, s->target = 148 * 4;
+  return true;
+}
+
+cudaError_t launch_paged_plan(const int* cu, const int* kv_len, int n_seq, int total_q, int max_q, int hq, int hkv, int dh,
+                              int causal, const PagedPlanShape& s, void* plan, int* err, cudaStream_t st) {
+  const PagedPlanBounds b = paged_plan_bounds(s, hkv, n_seq, total_q);
+  k_paged_plan<<<1, kPlanThreads, (n_seq + 1) * sizeof(int), st>>>(cu, kv_len, n_seq, total_q, max_q, hq, hkv, dh, causal, s, b,
+                                                                  plan, err);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_paged_join(const PagedAttnArgs& a, const PagedPlanShape& s, int max_joins, cudaStream_t st) {
+  const PagedPlanBounds b = paged_plan_bounds(s, a.c.hkv, a.n_seq, a.total_q);
+  PagedPlanHeader want{};
+  want.kind = s.kind, want.hq = a.hq, want.hkv = a.c.hkv, want.dh = a.c.dh, want.total_q = a.total_q, want.n_seq = a.n_seq;
+  want.max_q = a.max_q, want.rows = s.rows;
+  const long long threads = (long long)max_joins * a.c.hkv * (a.c.dh / 16) * s.rows * 8;
+  long long grid = (threads + 255) / 256;
+  if (grid > 148 * 8) grid = 148 * 8;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  // the kernel in front of it in the stream is the attention kernel of the same call
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_enabled() ? 1 : 0;
+  const PagedPlanHeader* hd = static_cast<const PagedPlanHeader*>(a.plan);
+  if (a.c.dtype == 1)
+    return cudaLaunchKernelEx(&cfg, k_paged_join<__nv_bfloat16>, want, hd, b.items, (const float*)a.ws,
+                              (__nv_bfloat16*)a.out, a.out_stride);
+  return cudaLaunchKernelEx(&cfg, k_paged_join<float>, want, hd, b.items, (const float*)a.ws, (float*)a.out, a.out_stride);
+}
+
+cudaError_t launch_paged_simt(const PagedAttnArgs& a, const PagedPlanShape& s, int grid, cudaStream_t st) {
+  const int dh = a.c.dh;
+#define PRISM_SIMT(T)                                                                     \
+  (s.rows == 16 ? (dh <= 64    ? simt_launch<T, 16, 4>(a, grid, st)                       \
+                   : dh <= 128 ? simt_launch<T, 16, 8>(a, grid, st)                       \
+                               : simt_launch<T, 16, 16>(a, grid, st))                     \
+                : (dh <= 64    ? simt_launch<T, 64, 4>(a, grid, st)                       \
+                   : dh <= 128 ? simt_launch<T, 64, 8>(a, grid, st)                       \
+                               : simt_launch<T, 64, 16>(a, grid, st)))
+  return a.c.dtype == 1 ? PRISM_SIMT(__nv_bfloat16) : PRISM_SIMT(float);
+#undef PRISM_SIMT
+}
+
+}  // namespace prism

@@ -21,6 +21,7 @@
 //
 // Every mbarrier wait is bounded: on expiry the kernel records kErrTimeout and all roles drain to
 // the common exit, which frees the tensor memory.  Every TMA load is a plain per-CTA load.
+#include "paged.cuh"
 #include "tc_common.cuh"
 
 namespace prism {
@@ -468,6 +469,23 @@ cudaError_t make_tma_2d_bf16(TmaDesc* out, const void* base, uint64_t rows, uint
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
   });
+}
+
+cudaError_t make_tma_nd_bf16(TmaDesc* out, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
+                             const uint32_t* box) {
+  EncodeTiledFn enc = get_encode();
+  if (!enc) return cudaErrorNotSupported;
+  if (rank < 2 || rank > 5 || (reinterpret_cast<uintptr_t>(base) & 15)) return cudaErrorInvalidValue;
+  cuuint64_t d[5], st[4];
+  cuuint32_t b[5], estr[5];
+  for (int i = 0; i < rank; ++i) {
+    d[i] = dims[i], b[i] = box[i], estr[i] = 1;
+    if (i) st[i - 1] = strides[i - 1];
+  }
+  const CUresult r = enc(reinterpret_cast<CUtensorMap*>(out), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
+                         const_cast<void*>(base), d, st, b, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
 int gemm_tc_sm_count() {

@@ -1,0 +1,159 @@
+// C entry points of the paged key/value cache (include/prism_ops.h): argument checks, then the launchers.
+#include "../../include/prism_ops.h"
+#include "paged.cuh"
+
+using namespace prism;
+
+namespace {
+int st_of(cudaError_t e) {
+  if (e == cudaSuccess) return PRISM_OK;
+  return e == cudaErrorMemoryAllocation ? PRISM_ERR_NOMEM : (e == cudaErrorInvalidValue ? PRISM_ERR_INVALID_ARG : PRISM_ERR_CUDA);
+}
+cudaStream_t S(void* s) { return reinterpret_cast<cudaStream_t>(s); }
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool page_size_ok(int32_t p) { return p >= 16 && p <= 256 && (p & (p - 1)) == 0; }
+// slots, and the tokens a block-table row can name, are counted in 32 bits
+bool pages_ok(int32_t num_pages, int32_t page_size) {
+  return num_pages >= 0 && page_size_ok(page_size) && ((int64_t)num_pages + 1) * page_size <= INT32_MAX;
+}
+int32_t elem(int32_t dtype) { return dtype == PRISM_BF16 ? 2 : 4; }
+
+int check_cache(const prism_kv_cache* c) {
+  if (!c || !c->k || !c->v || c->num_pages < 1 || c->n_kv_heads < 1) return PRISM_ERR_INVALID_ARG;
+  if (c->dtype != PRISM_FP32 && c->dtype != PRISM_BF16) return PRISM_ERR_INVALID_ARG;
+  if (!pages_ok(c->num_pages, c->page_size)) return PRISM_ERR_INVALID_ARG;
+  if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16) return PRISM_ERR_UNSUPPORTED;
+  if (c->n_kv_heads > 1024) return PRISM_ERR_UNSUPPORTED;
+  const int64_t page = (int64_t)c->n_kv_heads * c->page_size * c->head_dim;
+  if (c->page_stride < page || c->page_stride > ((int64_t)1 << 38) || (c->page_stride * elem(c->dtype)) % 16) return PRISM_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v)) return PRISM_ERR_INVALID_ARG;
+  return PRISM_OK;
+}
+PagedCache view(const prism_kv_cache* c) {
+  return PagedCache{c->k, c->v, (long long)c->page_stride, c->num_pages, c->page_size, c->n_kv_heads, c->head_dim, c->dtype};
+}
+
+// Shapes the attention entry points share.
+int check_shape(int32_t n_seq, int32_t total_q, int32_t max_q_len, int32_t hq, int32_t hkv, int32_t dh, int32_t dtype,
+                int32_t impl, PagedPlanShape* s) {
+  if (n_seq < 0 || total_q < 0 || max_q_len < 0 || hq < 1 || hkv < 1 || hq % hkv) return PRISM_ERR_INVALID_ARG;
+  if (dtype != PRISM_FP32 && dtype != PRISM_BF16) return PRISM_ERR_INVALID_ARG;
+  if (impl != PRISM_IMPL_AUTO && impl != PRISM_IMPL_SIMT) return PRISM_ERR_UNSUPPORTED;
+  if (n_seq > PRISM_MAX_CANDIDATES) return PRISM_ERR_SHAPE_LIMIT;
+  if (dh < 16 || dh > 256 || dh % 16 || hkv > 1024) return PRISM_ERR_UNSUPPORTED;
+  if (!paged_plan_shape(max_q_len, hq, hkv, dh, dtype, impl, s)) return PRISM_ERR_UNSUPPORTED;
+  // rows of the work list and of the grid are counted in 32 bits
+  if (paged_plan_bounds(*s, hkv, n_seq, total_q).items * hkv > INT32_MAX) return PRISM_ERR_SHAPE_LIMIT;
+  return PRISM_OK;
+}
+}  // namespace
+
+extern "C" {
+
+int prism_op_page_append(const int32_t* len_new, const int32_t* kv_len_in, int32_t* kv_len_out, int32_t n_seq, int32_t page_size,
+                         int32_t num_pages, int32_t max_pages, int64_t table_stride, int32_t* block_table,
+                         const int32_t* free_pages, const int32_t* n_free_in, int32_t* n_free_out, int32_t total, int32_t* cu_q,
+                         int32_t* pos, int32_t* slot_map, int32_t* err_word, void* stream) {
+  if (n_seq < 0 || total < 0 || max_pages < 0 || table_stride < max_pages || !pages_ok(num_pages, page_size) ||
+      !pages_ok(max_pages, page_size))
+    return PRISM_ERR_INVALID_ARG;
+  if (!n_free_in || !n_free_out || !cu_q || !err_word || (num_pages > 0 && !free_pages)) return PRISM_ERR_INVALID_ARG;
+  if (n_seq > 0 && (!len_new || !kv_len_in || !kv_len_out || (max_pages > 0 && !block_table))) return PRISM_ERR_INVALID_ARG;
+  if (total > 0 && (!pos || !slot_map)) return PRISM_ERR_INVALID_ARG;
+  if (n_seq > PRISM_MAX_CANDIDATES) return PRISM_ERR_SHAPE_LIMIT;
+  return st_of(launch_page_append(len_new, kv_len_in, kv_len_out, n_seq, page_size, num_pages, max_pages, table_stride,
+                                  block_table, free_pages, n_free_in, n_free_out, total, cu_q, pos, slot_map, err_word, S(stream)));
+}
+
+int prism_op_page_release(const int32_t* old_of_new, int32_t n_new, const int32_t* kv_len_in, int32_t* kv_len_out, int32_t n_seq,
+                          int32_t page_size, int32_t num_pages, int32_t shared_pages, int32_t max_pages, int64_t stride_in,
+                          const int32_t* table_in, int64_t stride_out, int32_t* table_out, int32_t* free_pages,
+                          const int32_t* n_free_in, int32_t* n_free_out, int32_t* err_word, void* stream) {
+  if (n_seq < 0 || n_new < 0 || n_new > n_seq || shared_pages < 0 || max_pages < 0 || stride_in < max_pages ||
+      stride_out < max_pages || !pages_ok(num_pages, page_size) || !pages_ok(max_pages, page_size))
+    return PRISM_ERR_INVALID_ARG;
+  if (!n_free_in || !n_free_out || !err_word || (num_pages > 0 && !free_pages)) return PRISM_ERR_INVALID_ARG;
+  if (n_seq > 0 && (!kv_len_in || !kv_len_out || (max_pages > 0 && (!table_in || !table_out)))) return PRISM_ERR_INVALID_ARG;
+  if (n_new > 0 && !old_of_new) return PRISM_ERR_INVALID_ARG;
+  if (n_seq > PRISM_MAX_CANDIDATES) return PRISM_ERR_SHAPE_LIMIT;
+  // rows move, so the two tables may not overlap
+  if (n_seq > 0 && max_pages > 0) {
+    const int32_t *a = table_in, *b = table_out;
+    if (a < b + (n_seq - 1) * stride_out + max_pages && b < a + (n_seq - 1) * stride_in + max_pages) return PRISM_ERR_INVALID_ARG;
+  }
+  return st_of(launch_page_release(old_of_new, n_new, kv_len_in, kv_len_out, n_seq, page_size, num_pages, shared_pages, max_pages,
+                                   stride_in, table_in, stride_out, table_out, free_pages, n_free_in, n_free_out, err_word,
+                                   S(stream)));
+}
+
+int prism_op_qknorm_rope_paged(const void* qkv, int64_t qkv_stride, const int32_t* pos, const int32_t* slot_map, int32_t rows,
+                               int32_t n_q_heads, int32_t qk_norm, const void* g_q, const void* g_k, float eps, float theta,
+                               void* q_out, int64_t q_stride, const prism_kv_cache* cache, int32_t* err_word, void* stream) {
+  if (int rc = check_cache(cache)) return rc;
+  if (rows < 0 || n_q_heads < 1 || n_q_heads > 4096 || !(theta > 0.f) || !err_word) return PRISM_ERR_INVALID_ARG;
+  if (qk_norm && (!g_q || !g_k || !aligned16(g_q) || !aligned16(g_k) || !(eps >= 0.f))) return PRISM_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)(n_q_heads + 2 * cache->n_kv_heads) * cache->head_dim, b = elem(cache->dtype);
+  if (qkv_stride < width || q_stride < (int64_t)n_q_heads * cache->head_dim || (qkv_stride * b) % 16 || (q_stride * b) % 16)
+    return PRISM_ERR_INVALID_ARG;
+  if (rows == 0) return PRISM_OK;
+  if (!qkv || !pos || !slot_map || !q_out || !aligned16(qkv) || !aligned16(q_out)) return PRISM_ERR_INVALID_ARG;
+  return st_of(launch_qknorm_rope_paged(qkv, qkv_stride, pos, slot_map, rows, n_q_heads, qk_norm, g_q, g_k, eps, theta, q_out,
+                                        q_stride, view(cache), err_word, S(stream)));
+}
+
+int prism_op_attention_paged_bytes(int32_t n_seq, int32_t total_q, int32_t max_q_len, int32_t n_q_heads, int32_t n_kv_heads,
+                                   int32_t head_dim, int32_t dtype, int32_t impl, int64_t* plan_bytes, int64_t* workspace_bytes) {
+  PagedPlanShape s;
+  if (!plan_bytes || !workspace_bytes) return PRISM_ERR_INVALID_ARG;
+  if (int rc = check_shape(n_seq, total_q, max_q_len, n_q_heads, n_kv_heads, head_dim, dtype, impl, &s)) return rc;
+  const PagedPlanBounds b = paged_plan_bounds(s, n_kv_heads, n_seq, total_q);
+  *plan_bytes = paged_plan_bytes(b);
+  *workspace_bytes = paged_ws_bytes(s, b, n_kv_heads, head_dim);
+  return PRISM_OK;
+}
+
+int prism_op_attention_paged_plan(const int32_t* cu_q, const int32_t* kv_len, int32_t n_seq, int32_t total_q, int32_t max_q_len,
+                                  int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t causal,
+                                  int32_t impl, void* plan, int64_t plan_bytes, int32_t* err_word, void* stream) {
+  PagedPlanShape s;
+  if (int rc = check_shape(n_seq, total_q, max_q_len, n_q_heads, n_kv_heads, head_dim, dtype, impl, &s)) return rc;
+  if (!plan || !aligned16(plan) || !err_word || !cu_q || (n_seq > 0 && !kv_len)) return PRISM_ERR_INVALID_ARG;
+  if (plan_bytes < paged_plan_bytes(paged_plan_bounds(s, n_kv_heads, n_seq, total_q))) return PRISM_ERR_INVALID_ARG;
+  return st_of(launch_paged_plan(cu_q, kv_len, n_seq, total_q, max_q_len, n_q_heads, n_kv_heads, head_dim, causal ? 1 : 0, s, plan,
+                                 err_word, S(stream)));
+}
+
+int prism_op_attention_paged(const void* q, int64_t q_stride, const prism_kv_cache* cache, const int32_t* block_table,
+                             int64_t table_stride, int32_t max_pages, const void* plan, int64_t plan_bytes, int32_t n_seq,
+                             int32_t total_q, int32_t max_q_len, int32_t n_q_heads, int32_t impl, void* out, int64_t out_stride,
+                             void* workspace, int64_t workspace_bytes, int32_t* err_word, void* stream) {
+  if (int rc = check_cache(cache)) return rc;
+  PagedPlanShape s;
+  const int32_t hkv = cache->n_kv_heads, dh = cache->head_dim, b = elem(cache->dtype);
+  if (int rc = check_shape(n_seq, total_q, max_q_len, n_q_heads, hkv, dh, cache->dtype, impl, &s)) return rc;
+  if (max_pages < 0 || table_stride < max_pages || !pages_ok(max_pages, cache->page_size) || !err_word) return PRISM_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)n_q_heads * dh;
+  if (q_stride < width || out_stride < width || (q_stride * b) % 16 || (out_stride * b) % 16 || q_stride > ((int64_t)1 << 38))
+    return PRISM_ERR_INVALID_ARG;
+  const PagedPlanBounds bound = paged_plan_bounds(s, hkv, n_seq, total_q);
+  if (!plan || !aligned16(plan) || plan_bytes < paged_plan_bytes(bound)) return PRISM_ERR_INVALID_ARG;
+  // A tile is cut only if its keys, which the table's width bounds, are more than the shortest piece.
+  const int64_t max_keys = (int64_t)max_pages * cache->page_size;
+  const bool may_cut = max_keys > s.min_piece;
+  if (may_cut && (!workspace || !aligned16(workspace) || workspace_bytes < paged_ws_bytes(s, bound, hkv, dh))) return PRISM_ERR_INVALID_ARG;
+  if (n_seq == 0 || total_q == 0 || max_q_len == 0) return PRISM_OK;
+  if (!q || !out || !aligned16(q) || !aligned16(out) || (max_pages > 0 && !block_table)) return PRISM_ERR_INVALID_ARG;
+  PagedAttnArgs a;
+  a.q = q, a.q_stride = q_stride, a.c = view(cache), a.table = block_table, a.max_pages = max_pages, a.table_stride = table_stride;
+  a.plan = plan, a.n_seq = n_seq, a.total_q = total_q, a.max_q = max_q_len, a.hq = n_q_heads, a.out = out, a.out_stride = out_stride;
+  a.ws = may_cut ? static_cast<float*>(workspace) : nullptr, a.err = err_word;
+  const int64_t tiles = (int64_t)total_q / s.tokens + n_seq;
+  const int grid = (int)((may_cut ? bound.items : tiles) * hkv);
+  cudaError_t e = s.kind == kPagedTokens  ? launch_paged_tokens(a, s, grid, S(stream))
+                  : s.kind == kPagedTiles ? launch_paged_tiles(a, s, grid, S(stream))
+                                          : launch_paged_simt(a, s, grid, S(stream));
+  if (e == cudaSuccess && may_cut) e = launch_paged_join(a, s, (int)bound.joins, S(stream));
+  return st_of(e);
+}
+
+}  // extern "C"

@@ -54,6 +54,19 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int* er
   return true;
 }
 
+// The same for a whole warp in step: every lane waits, and all of them get the same answer, so that no lane can leave for
+// the exit while the others go on to a warp-wide instruction.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, int* err, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, err, abort_flag));
+}
+// Wait for a phase on the way out: nothing but its own limit ends it early, so that copies and MMAs in flight land before
+// the memory they write is given back, also after some other wait gave up.
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, unsigned long long limit = kWaitCycles) {
+  const unsigned long long t0 = clock64();
+  while (!mbar_try(bar, parity))
+    if (clock64() - t0 > limit) return;
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"

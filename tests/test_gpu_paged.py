@@ -1,0 +1,690 @@
+"""-m gpu: the paged key/value cache through the C ABI (prism_op_page_*, _qknorm_rope_paged, _attention_paged*) against plain
+64-bit forms.  Tolerances are derived in paged_reference.attention_tolerance and beside each use."""
+import numpy as np
+import pytest
+
+from paged_reference import append, attention, attention_tolerance, norm_rope, pages_of, release
+from synth.weights import round_to_bf16
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+FP32, BF16 = 0, 1
+AUTO, SIMT = 0, 1
+
+
+@pytest.fixture(scope="module")
+def P():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA device")
+    import paper_2510_15620_b200 as pkg
+    return pkg
+
+
+def i32(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+
+def err_word():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def tdt(dtype):
+    return torch.bfloat16 if dtype == BF16 else torch.float32
+
+
+def draw(rng, dtype, *shape):
+    x = rng.normal(size=shape).astype(np.float32)
+    return round_to_bf16(x) if dtype == BF16 else x
+
+
+def dev(a, dtype):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(tdt(dtype)).cuda()
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+# ------------------------------------------------------------------------------------------------ pages
+def random_pool(rng, lens, page, extra, max_pages, shared=0):
+    """A table for sequences of these lengths, and the stack of free pages."""
+    need = [max(0, pages_of(int(n), page) - shared) for n in lens]
+    pool = sum(need) + shared + extra
+    perm = rng.permutation(pool)
+    table = np.full((len(lens), max_pages), -1, np.int64)
+    at = shared
+    for s, k in enumerate(need):
+        table[s, :min(shared, pages_of(int(lens[s]), page))] = perm[:min(shared, pages_of(int(lens[s]), page))]
+        table[s, shared:shared + k] = perm[at:at + k]
+        at += k
+    free = np.full(pool, -5, np.int64)
+    free[:pool - at] = perm[at:]
+    return table, free, pool - at, pool
+
+
+APPENDS = [(1, 16, [0], [1]), (1, 16, [15], [1]), (1, 16, [16], [1]), (3, 32, [0, 5, 64], [0, 0, 0]),
+           (4, 64, [1, 63, 64, 65], [64, 1, 0, 200]), (300, 128, (0, 400), (0, 300)), (4096, 16, (0, 40), (0, 9)),
+           (1, 256, [100], [70001])]
+
+
+def append_inputs(n, page, cached, new):
+    rng = np.random.default_rng(n + page)
+    kv = np.array(cached) if isinstance(cached, list) else rng.integers(*cached, size=n)
+    add = np.array(new) if isinstance(new, list) else rng.integers(*new, size=n)
+    extra = int((pages_of(kv + add, page) - pages_of(kv, page)).sum())
+    max_pages = int(pages_of(kv + add, page).max()) + 2
+    return rng, kv, add, random_pool(rng, kv, page, extra + 3, max_pages)
+
+
+def call_append(P, kv, add, page, pool, table, free, n_free, total, in_place=False, err=None):
+    kv_in, nf = i32(kv), i32([n_free])
+    o = dict(kv=kv_in if in_place else i32(np.full(len(kv), -9)), nf=nf if in_place else i32([-9]), table=i32(table),
+             free=i32(free), cu=i32(np.full(len(kv) + 1, -9)), pos=i32(np.full(total, -9)), slot=i32(np.full(total, -9)))
+    err = err_word() if err is None else err
+    P.ops.prism_op_page_append(i32(add), kv_in, o["kv"], page, pool, o["table"], o["free"], nf, o["nf"], o["cu"], o["pos"],
+                               o["slot"], err)
+    torch.cuda.synchronize()
+    return {k: v.cpu().numpy() for k, v in o.items()}, int(err.item())
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("n,page,cached,new", APPENDS)
+def test_append(P, n, page, cached, new, in_place):
+    rng, kv, add, (table, free, n_free, pool) = append_inputs(n, page, cached, new)
+    total = int(add.sum()) + 5                       # five padding rows
+    got, err = call_append(P, kv, add, page, pool, table, free, n_free, total, in_place)
+    want = append(kv_len=kv, len_new=add, page=page, table=table, free=free, n_free=n_free, total=total)
+    assert err == 0
+    for key, w in zip(("kv", "table", "nf", "cu", "pos", "slot"), want):
+        assert np.array_equal(got[key].ravel(), np.asarray(w).ravel()), key
+    assert np.array_equal(got["free"], free)
+
+
+def test_append_uses_the_last_page_and_no_sequences(P):
+    got, err = call_append(P, np.array([0, 16]), np.array([16, 1]), 16, 3, np.array([[-1, -1], [2, -1]]), np.array([0, 1, 7]), 2, 17)
+    assert err == 0 and got["nf"][0] == 0 and got["table"].tolist() == [[1, -1], [2, 0]] and got["slot"][-1] == 0
+    got, err = call_append(P, np.zeros(0, int), np.zeros(0, int), 16, 3, np.zeros((0, 2), int), np.array([0, 1, 2]), 3, 4)
+    assert err == 0 and got["nf"][0] == 3 and got["cu"].tolist() == [0] and got["slot"].tolist() == [-1] * 4
+
+
+@pytest.mark.parametrize("case", ["pool", "row", "negative_new", "negative_old", "total", "count"])
+def test_append_refused_as_a_whole(P, case):
+    rng, kv, add, (table, free, n_free, pool) = append_inputs(4, 64, [1, 63, 64, 65], [64, 1, 0, 200])
+    total, bit = int(add.sum()), 2
+    if case == "pool":
+        n_free, bit = 1, 32
+    elif case == "count":
+        n_free, bit = pool + 1, 32
+    elif case == "row":
+        add, total = add.copy(), 4000
+        add[3] = table.shape[1] * 64 - 64
+    elif case == "negative_new":
+        add = np.array([64, -1, 0, 200])
+    elif case == "negative_old":
+        kv = np.array([1, 63, -64, 65])
+    else:
+        total -= 1
+    got, err = call_append(P, kv, add, 64, pool, table, free, n_free, total)
+    assert err == bit
+    assert np.array_equal(got["kv"], kv) and got["nf"][0] == n_free and np.array_equal(got["table"], table)
+    assert not got["cu"].any() and (got["slot"] == -1).all() and not got["pos"].any()
+
+
+def test_append_marks_page_ids_outside_the_cache(P):
+    # the first sequence's half-filled page and the second one's new page are outside
+    got, err = call_append(P, np.array([8, 0, 0]), np.array([2, 3, 1]), 16, 6, np.array([[9, -1], [-1, -1], [-1, -1]]),
+                           np.array([0, 1, 2, 4, 77, 0]), 5, 6)
+    assert err == 16
+    assert got["table"].tolist() == [[9, -1], [-1, -1], [4, -1]]
+    assert got["slot"].tolist() == [-1, -1, -1, -1, -1, 64] and got["pos"].tolist() == [8, 9, 0, 1, 2, 0]
+
+
+def call_release(P, keep, kv, page, pool, shared, table, free, n_free, in_place=False):
+    kv_in, nf = i32(kv), i32([n_free])
+    o = dict(kv=kv_in if in_place else i32(np.full(len(kv), -9)), table=i32(np.full(table.shape, -9)), free=i32(free),
+             nf=nf if in_place else i32([-9]))
+    err = err_word()
+    P.ops.prism_op_page_release(i32(keep) if len(keep) else torch.empty(0, dtype=torch.int32, device="cuda"), kv_in, o["kv"], page,
+                                pool, shared, i32(table), o["table"], o["free"], nf, o["nf"], err)
+    torch.cuda.synchronize()
+    return {k: v.cpu().numpy() for k, v in o.items()}, int(err.item())
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("n,keep,page,shared,lens", [(1, 0, 16, 0, (0, 50)), (1, 1, 16, 0, (1, 50)), (100, 40, 16, 2, (32, 600)),
+                                                     (5, 5, 64, 1, (64, 65)), (4096, 1000, 128, 0, (0, 2000)),
+                                                     (33, 0, 256, 3, (768, 5000))])
+def test_release(P, n, keep, page, shared, lens, in_place):
+    rng = np.random.default_rng(n + keep)
+    kv = rng.integers(lens[0], lens[1], size=n)
+    max_pages = int(pages_of(kv.max(), page)) + 4
+    table, free, n_free, pool = random_pool(rng, kv, page, 7, max_pages, shared)
+    kept = rng.permutation(n)[:keep]                 # any order
+    got, err = call_release(P, kept, kv, page, pool, shared, table, free, n_free, in_place)
+    want = release(kept.tolist(), kv, page, shared, table, free, n_free)
+    assert err == 0
+    for key, w in zip(("kv", "table", "free", "nf"), want):
+        assert np.array_equal(got[key].ravel(), np.asarray(w).ravel()), key
+
+
+@pytest.mark.parametrize("case", ["twice", "outside", "length", "long", "full"])
+def test_release_refused_as_a_whole(P, case):
+    rng = np.random.default_rng(8)
+    kv = np.array([40, 16, 0, 33])
+    table, free, n_free, pool = random_pool(rng, kv, 16, 2, 4)
+    keep, bit = [0, 2], 2
+    if case == "twice":
+        keep = [2, 2]
+    elif case == "outside":
+        keep = [0, 4]
+    elif case == "length":
+        kv = np.array([40, -1, 0, 33])
+    elif case == "long":
+        kv = np.array([40, 65, 0, 33])
+    else:
+        n_free, bit = pool - 1, 32
+    got, err = call_release(P, np.array(keep), kv, 16, pool, 0, table, free, n_free)
+    assert err == bit
+    assert np.array_equal(got["kv"], kv) and got["nf"][0] == n_free
+    assert np.array_equal(got["table"], table) and np.array_equal(got["free"], free)
+
+
+def test_append_after_release_takes_the_pages_back(P):
+    rng = np.random.default_rng(3)
+    kv = rng.integers(1, 300, size=50)
+    table, free, n_free, pool = random_pool(rng, kv, 16, 0, 48)
+    assert n_free == 0
+    keep = np.sort(rng.permutation(50)[:20])
+    got, err = call_release(P, keep, kv, 16, pool, 0, table, free, n_free)
+    assert err == 0
+    room = int(got["nf"][0])
+    add = np.zeros(50, int)
+    add[:20] = 16 * (room // 20)
+    after, err = call_append(P, got["kv"], add, 16, pool, got["table"], got["free"], room, int(add.sum()))
+    assert err == 0
+    owned = [p for s in range(20) for p in after["table"][s, :pages_of(int(after["kv"][s]), 16)]]
+    owned += after["free"][:after["nf"][0]].tolist()
+    assert sorted(owned) == list(range(pool))        # every page is owned once or free once
+
+
+# ------------------------------------------------------------------------------------------------ norm + rotation
+ROPES = [(1, 16, 8, 128, BF16, 1, 16), (773, 4, 2, 64, FP32, 0, 16), (130, 4, 2, 64, FP32, 1, 32), (77, 28, 4, 128, BF16, 1, 64),
+         (33, 3, 1, 80, BF16, 1, 128), (65, 8, 8, 256, FP32, 1, 256), (19, 1, 1, 16, BF16, 1, 16), (19, 5, 5, 16, FP32, 0, 16),
+         (40, 32, 8, 96, FP32, 1, 16), (21, 2, 1, 256, BF16, 0, 16)]
+
+
+@pytest.mark.parametrize("rows,hq,hkv,dh,dtype,norm,page", ROPES)
+@pytest.mark.parametrize("in_place", [False, True])
+def test_norm_rotation_and_cache_rows(P, rows, hq, hkv, dh, dtype, norm, page, in_place):
+    rng = np.random.default_rng(rows + dh)
+    theta, width, q_width = 1e6, (hq + 2 * hkv) * dh, hq * dh
+    x = draw(rng, dtype, rows, width)
+    gq, gk = 1 + draw(rng, dtype, dh) * 0.125, 1 + draw(rng, dtype, dh) * 0.125
+    if dtype == BF16:
+        gq, gk = round_to_bf16(gq), round_to_bf16(gk)
+    pos = rng.integers(0, 1 << 20, size=rows)
+    pages = pages_of(rows, page) + 3
+    slots = rng.permutation(pages * page)[:rows]
+    slots[rng.integers(0, rows, size=rows // 9)] = -1            # padding rows
+    k0, v0 = draw(rng, dtype, pages, hkv, page, dh), draw(rng, dtype, pages, hkv, page, dh)
+    wide = torch.full((rows, width + 24), 7.0, dtype=tdt(dtype), device="cuda")
+    qkv = wide[:, 8:8 + width]                                   # rows with a stride, not at the start of the buffer
+    qkv.copy_(dev(x, dtype))
+    q = qkv[:, :q_width] if in_place else torch.full((rows, q_width + 16), 5.0, dtype=tdt(dtype), device="cuda")[:, :q_width]
+    before = host(q)
+    arena = torch.stack([dev(k0, dtype), dev(v0, dtype)], 1)     # pages hold keys, then values: one stride for both
+    err = err_word()
+    P.ops.prism_op_qknorm_rope_paged(qkv, dtype, i32(pos), i32(slots), hq, norm, dev(gq, dtype), dev(gk, dtype), 1e-6, theta, q,
+                                     arena[:, 0], arena[:, 1], err)
+    torch.cuda.synchronize()
+    assert int(err.item()) == 0
+    xs = x.astype(np.float64).reshape(rows, hq + 2 * hkv, dh)
+    want_q, size_q = norm_rope(xs[:, :hq], pos, gq.astype(np.float64) if norm else None, 1e-6, np.float64(np.float32(theta)))
+    want_k, size_k = norm_rope(xs[:, hq:hq + hkv], pos, gk.astype(np.float64) if norm else None, 1e-6, np.float64(np.float32(theta)))
+    want_v = xs[:, hq + hkv:]
+    # fp32 inside: the sum of dh squares (dh 2^-24 relative, halved by the root), root, quotient, two products of the norm,
+    # sine and cosine (within 2^-22 each), two products and a sum: (dh / 2 + 16) 2^-24 of |a| + |b|; then one rounding
+    half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    tol = lambda w, size: half * np.abs(w) + (1 + half) * (dh / 2 + 16) * 2.0 ** -24 * size + 1e-30
+    live = slots >= 0
+    got_q = host(q).reshape(rows, hq, dh)
+    assert (np.abs(got_q - want_q) <= tol(want_q, size_q))[live].all()
+    assert np.array_equal(got_q[~live], before.reshape(rows, hq, dh)[~live])
+    k, v = k0.astype(np.float64), v0.astype(np.float64)
+    page_of, off = slots[live] // page, slots[live] % page
+    bound = np.zeros_like(k)
+    k[page_of, :, off], v[page_of, :, off] = want_k[live], want_v[live]
+    bound[page_of, :, off] = tol(want_k, size_k)[live]
+    assert (np.abs(host(arena[:, 0]) - k) <= bound).all()       # untouched rows: bit for bit
+    assert np.array_equal(host(arena[:, 1]), v)
+    rest = host(wide)
+    assert (rest[:, :8] == 7).all() and (rest[:, 8 + width:] == 7).all()
+    assert np.array_equal(rest[:, 8 + q_width:8 + width], x[:, q_width:].astype(np.float64))
+
+
+def test_rotation_of_far_and_equal_positions(P):
+    """Positions up to 2^31 - 1 against numpy's 64-bit angles, and the same row at the same position twice: the same bits."""
+    rows, dh = 64, 128
+    rng = np.random.default_rng(0)
+    x = np.repeat(draw(rng, FP32, rows // 2, 3 * dh), 2, 0)
+    pos = np.repeat(np.concatenate([[0, 1, 2 ** 31 - 1, 2 ** 24 + 1], rng.integers(0, 2 ** 31, size=28)]), 2)
+    cache = torch.zeros(2, 8, 1, 16, dh, device="cuda")
+    q, err = torch.empty(rows, dh, device="cuda"), err_word()
+    P.ops.prism_op_qknorm_rope_paged(dev(x, FP32), FP32, i32(pos), i32(np.arange(rows)), 1, 0, None, None, 0.0, 1e4, q, cache[0],
+                                     cache[1], err)
+    got = host(q)
+    assert np.array_equal(got[::2], got[1::2])
+    want, size = norm_rope(x[:, :dh].astype(np.float64)[:, None], pos, None, 0.0, 1e4)
+    # angles: pos * frequency in 64 bits on both sides, 2^31 * 2^-52 apart at most; then (dh / 2 + 16) 2^-24 as above
+    tol = (2.0 ** 31 * 2.0 ** -52 + (dh / 2 + 16) * 2.0 ** -24) * size[:, 0] + 2.0 ** -24 * np.abs(want[:, 0])
+    assert (np.abs(got - want[:, 0]) <= tol).all()
+
+
+def test_rotation_refuses_slots_outside_the_cache(P):
+    x = torch.ones(3, 3 * 64, device="cuda")
+    q, err = torch.full((3, 64), 9.0, device="cuda"), err_word()
+    cache = torch.zeros(2, 2, 1, 16, 64, device="cuda")
+    P.ops.prism_op_qknorm_rope_paged(x, FP32, i32([0, 0, 0]), i32([32, 31, 1 << 30]), 1, 0, None, None, 0.0, 1e4, q, cache[0], cache[1],
+                                     err)
+    torch.cuda.synchronize()
+    assert int(err.item()) == 16
+    assert (q[0] == 9).all() and (q[1] == 1).all() and (q[2] == 9).all()
+    assert cache.sum().item() == 128 and (cache[:, 1, 0, 15] == 1).all()
+
+
+# ------------------------------------------------------------------------------------------------ attention
+class Call:
+    """One attention call with everything a user holds; unused pages, unused rows of last pages and the rows of q and out
+    around the sequences are NaN."""
+
+    def __init__(self, P, rng, new, kv, hq, hkv, dh, dtype, causal, page, scale=1.0, impl=AUTO, lead=2, trail=3, shared=0,
+                 max_q=None, wide=0, need_ws=True):
+        self.P, self.impl, self.dtype, self.hq, self.causal = P, impl, dtype, hq, causal
+        new, kv = np.asarray(new), np.asarray(kv)
+        self.new, self.kv, n = new, kv, len(new)
+        self.cu = lead + np.concatenate([[0], np.cumsum(new)])
+        rows = int(self.cu[-1]) + trail
+        max_pages = max(1, int(pages_of(kv.max(initial=0), page))) + wide
+        self.table, _, _, pool = random_pool(rng, kv, page, 4, max_pages, shared)
+        self.q = draw(rng, dtype, rows, hq, dh) * scale
+        if dtype == BF16:
+            self.q = round_to_bf16(self.q)
+        self.k, self.v = draw(rng, dtype, pool, hkv, page, dh), draw(rng, dtype, pool, hkv, page, dh)
+        k, v = np.full_like(self.k, np.nan), np.full_like(self.v, np.nan)
+        for s in range(n):
+            for t in range(int(kv[s])):
+                p, r = self.table[s, t // page], t % page
+                k[p, :, r], v[p, :, r] = self.k[p, :, r], self.v[p, :, r]
+        q = self.q.copy()
+        q[:lead], q[rows - trail:] = np.nan, np.nan
+        arena = torch.stack([dev(k, dtype), dev(v, dtype)], 1)
+        self.kd, self.vd = arena[:, 0], arena[:, 1]
+        qd = torch.full((rows, hq * dh + 16), float("nan"), dtype=tdt(dtype), device="cuda")
+        self.qd = qd[:, 8:8 + hq * dh]
+        self.qd.copy_(dev(q.reshape(rows, -1), dtype))
+        self.outd = torch.full((rows, hq * dh + 24), 3.0, dtype=tdt(dtype), device="cuda")
+        self.tabled, self.cud, self.kvd, self.err = i32(self.table), i32(self.cu), i32(kv), err_word()
+        self.max_q = int(new.max(initial=0)) if max_q is None else max_q
+        pb, wb = P.ops.prism_op_attention_paged_bytes(n, rows, self.max_q, hq, hkv, dh, dtype, impl)
+        self.plan = torch.full((pb,), 255, dtype=torch.uint8, device="cuda")
+        self.ws = torch.full((wb,), 255, dtype=torch.uint8, device="cuda") if need_ws else None   # NaN in every word
+        self.hkv, self.dh, self.n = hkv, dh, n
+
+    @property
+    def out(self):
+        return self.outd[:, 16:16 + self.hq * self.dh]
+
+    def make_plan(self):
+        self.P.ops.prism_op_attention_paged_plan(self.cud, self.kvd, self.qd.shape[0], self.max_q, self.hq, self.hkv, self.dh,
+                                                 self.dtype, self.causal, self.plan, self.err, self.impl)
+
+    def attend(self):
+        self.P.ops.prism_op_attention_paged(self.qd, self.kd, self.vd, self.tabled, self.plan, self.n, self.max_q, self.hq, self.dtype,
+                                            self.out, self.ws, self.err, self.impl)
+
+    def check(self):
+        torch.cuda.synchronize()
+        assert int(self.err.item()) == 0
+        rows = self.qd.shape[0]
+        out, avg, size = attention(self.q.astype(np.float64), self.k.astype(np.float64), self.v.astype(np.float64), self.table,
+                                   self.cu, self.kv, self.causal)
+        tol = attention_tolerance(out, avg, size, self.dh, int(self.kv.max(initial=0)), self.dtype == BF16)
+        got = host(self.out).reshape(rows, self.hq, self.dh)
+        a, b = int(self.cu[0]), int(self.cu[-1])
+        bad = ~(np.abs(got - out) <= tol)[a:b]
+        assert not bad.any(), (np.argwhere(bad)[:5], float(np.nanmax((np.abs(got - out) / tol)[a:b])))
+        all_out = host(self.outd)
+        assert (all_out[:a] == 3).all() and (all_out[b:] == 3).all()          # rows of no sequence
+        assert (all_out[:, :16] == 3).all() and (all_out[:, 16 + self.hq * self.dh:] == 3).all()
+        return self
+
+    def run(self):
+        self.make_plan()
+        self.attend()
+        return self.check()
+
+
+TOKENS = [  # one to a few new tokens, at most 16 (token, head) rows: lengths around page, stage and piece borders
+    (16, 8, 128, 16, [1] * 9, [1, 2, 15, 16, 17, 63, 64, 65, 300]),
+    (32, 8, 128, 64, [1, 4, 2, 0, 3], [70, 4, 1, 50, 999]),                 # q_len 2 of 1 key: a row that sees nothing
+    (16, 16, 64, 16, [1, 1, 16, 7], [0, 33, 20, 129]),                      # no keys at all
+    (8, 1, 64, 32, [1, 2, 1], [31, 2100, 5000]),                            # cut into pieces
+    (16, 1, 128, 128, [1, 1], [127, 3001]),
+    (12, 4, 128, 256, [5, 1], [256, 777]),
+]
+TILES = [  # chunks
+    (16, 8, 128, 16, [17, 64, 65, 1, 128, 129], [17, 100, 65, 40, 500, 129]),
+    (32, 8, 128, 64, [33, 64, 5, 0, 70], [40, 1200, 2500, 9, 3]),           # more rows than keys
+    (16, 16, 64, 16, [130, 300, 1], [130, 700, 0]),
+    (28, 4, 128, 32, [36, 37, 18], [36, 2200, 400]),                        # 18 tokens a tile, two rows of it idle
+    (12, 4, 64, 128, [43, 84, 90], [128, 129, 2000]),
+    (8, 1, 128, 256, [16, 33, 200], [257, 511, 1500]),
+    (128, 1, 64, 16, [1, 2, 3], [5, 1100, 2050]),                           # one token a tile
+]
+
+
+@pytest.mark.parametrize("causal", [1, 0])
+@pytest.mark.parametrize("case", range(len(TOKENS)))
+def test_attention_of_few_tokens(P, case, causal):
+    hq, hkv, dh, page, new, kv = TOKENS[case]
+    rng = np.random.default_rng(case)
+    Call(P, rng, new, kv, hq, hkv, dh, BF16, causal, page).run()
+
+
+@pytest.mark.parametrize("causal", [1, 0])
+@pytest.mark.parametrize("case", range(len(TILES)))
+def test_attention_of_chunks(P, case, causal):
+    hq, hkv, dh, page, new, kv = TILES[case]
+    rng = np.random.default_rng(10 + case)
+    Call(P, rng, new, kv, hq, hkv, dh, BF16, causal, page).run()
+
+
+@pytest.mark.parametrize("causal", [1, 0])
+@pytest.mark.parametrize("dtype,impl,hq,hkv,dh,page,new,kv", [
+    (FP32, AUTO, 4, 2, 64, 16, [16, 1, 0, 48], [16, 33, 7, 64]),
+    (FP32, AUTO, 16, 8, 128, 16, [1, 1, 3], [0, 700, 2]),
+    (FP32, AUTO, 28, 4, 128, 64, [20, 40], [1000, 41]),
+    (FP32, AUTO, 2, 2, 256, 32, [5, 70], [600, 70]),
+    (FP32, AUTO, 64, 1, 16, 16, [1, 2], [64, 900]),
+    (FP32, AUTO, 6, 2, 80, 128, [9, 1], [300, 1]),
+    (BF16, AUTO, 6, 2, 80, 16, [9, 40], [300, 41]),
+    (BF16, AUTO, 2, 1, 256, 16, [1, 3], [700, 20]),
+    (BF16, SIMT, 16, 8, 128, 16, [33, 1], [400, 65]),
+    (BF16, SIMT, 16, 8, 64, 16, [1, 2], [400, 65])])
+def test_attention_on_cuda_cores(P, dtype, impl, hq, hkv, dh, page, new, kv, causal):
+    rng = np.random.default_rng(dh + hq)
+    Call(P, rng, new, kv, hq, hkv, dh, dtype, causal, page, impl=impl).run()
+
+
+@pytest.mark.parametrize("new", [[1, 2, 4], [40, 70, 130]])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_attention_with_scores_far_apart(P, new, dtype):
+    """Scores hundreds of powers of two apart: references move inside a block, between blocks and between pieces."""
+    rng = np.random.default_rng(5)
+    c = Call(P, rng, new, [60, 700, 2600], 16, 8, 128, dtype, 1, 16, scale=64.0)
+    c.run()
+
+
+def test_attention_with_a_growing_and_a_falling_score(P):
+    """Keys whose scores rise (or fall) steadily over the sequence, by far more than fp32 exponents hold."""
+    for new in ([1], [64]):
+        for sign in (1.0, -1.0):
+            rng = np.random.default_rng(6)
+            c = Call(P, rng, new, [1500], 16, 8, 128, BF16, 1, 16)
+            ramp = round_to_bf16((sign * np.linspace(0, 60, 1500)).astype(np.float32))
+            for t in range(1500):
+                p, r = c.table[0, t // 16], t % 16
+                c.k[p, :, r, 0] = ramp[t]
+            c.q[:, :, 0] = 100.0
+            c.kd.copy_(dev(c.k, BF16))
+            c.qd.copy_(dev(c.q.reshape(c.q.shape[0], -1), BF16))
+            c.run()
+
+
+def test_attention_over_a_shared_prefix_and_many_sequences(P):
+    rng = np.random.default_rng(9)
+    new = rng.integers(0, 90, size=150)
+    Call(P, rng, new, 64 + new, 16, 8, 128, BF16, 1, 16, shared=4).run()
+    new = rng.integers(0, 2, size=1000)
+    Call(P, rng, new, new + rng.integers(0, 150, size=1000), 32, 8, 128, BF16, 1, 32).run()
+
+
+def test_attention_table_wider_than_needed_and_max_q_above_the_longest(P):
+    rng = np.random.default_rng(2)
+    Call(P, rng, [1, 2], [50, 90], 16, 8, 128, BF16, 1, 16, wide=500).run()
+    Call(P, rng, [1, 2], [50, 90], 16, 8, 128, BF16, 1, 16, max_q=300).run()      # the chunk kernel on single tokens
+    Call(P, rng, [1, 1], [50, 200], 16, 8, 128, BF16, 1, 16, need_ws=False).run()  # too narrow to be cut: no workspace
+
+
+def test_attention_results_repeat_bit_for_bit(P):
+    for new, kv in (([1, 1, 1], [5000, 100, 777]), ([100, 300], [4000, 300])):
+        c = Call(P, np.random.default_rng(4), new, kv, 16, 8, 128, BF16, 1, 16).run()
+        first = c.outd.clone()
+        for _ in range(5):
+            c.out.fill_(1.0)
+            c.outd[:, :16] = 3.0
+            c.attend()
+            torch.cuda.synchronize()
+            a, b = int(c.cu[0]), int(c.cu[-1])
+            assert torch.equal(first[a:b], c.outd[a:b])
+
+
+def test_attention_captured_and_replayed_with_new_lengths(P):
+    """Plan and attention in a graph: the replay reads whatever lengths, tables and rows are there then."""
+    rng = np.random.default_rng(12)
+    for new, kv, kv2 in (([1, 1, 1], [40, 900, 3], [700, 12, 333]), ([60, 20, 3], [60, 900, 3], [200, 21, 500])):
+        c = Call(P, rng, new, np.maximum(kv, kv2), 16, 8, 128, BF16, 1, 16)
+        full = c.kv.copy()
+        c.run()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.make_plan()
+            c.attend()
+        for lens in (kv, kv2, full):
+            c.kv = np.asarray(lens)
+            c.kvd.copy_(i32(lens))
+            c.outd.fill_(3.0)
+            g.replay()
+            c.check()
+        del g
+
+
+def test_two_calls_at_once_share_a_plan_but_not_a_workspace(P):
+    for new, kv in (([1, 1], [9000, 4000]), ([70, 20], [6000, 2500])):
+        c = Call(P, np.random.default_rng(13), new, kv, 16, 8, 128, BF16, 1, 16)
+        c.run()
+        want = c.outd.clone()
+        ws2, out2 = c.ws.clone(), torch.full_like(c.outd, 3.0)
+        s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        for _ in range(10):
+            with torch.cuda.stream(s1):
+                c.attend()
+            with torch.cuda.stream(s2):
+                P.ops.prism_op_attention_paged(c.qd, c.kd, c.vd, c.tabled, c.plan, c.n, c.max_q, c.hq, BF16,
+                                               out2[:, 16:16 + c.hq * c.dh], ws2, c.err)
+        torch.cuda.synchronize()
+        assert torch.equal(c.outd, want) and torch.equal(out2, want)
+
+
+def test_attention_reports_bad_pages_and_plans(P):
+    for new in ([1, 1], [40, 1]):
+        rng = np.random.default_rng(21)
+        c = Call(P, rng, new, [50, 300], 16, 8, 128, BF16, 1, 16).run()
+        c.tabled[1, 3] = 1 << 30                                   # outside the cache
+        c.attend()
+        torch.cuda.synchronize()
+        assert int(c.err.item()) == 16
+        c.err.zero_()
+        c.tabled[1, 3] = -1
+        c.attend()
+        torch.cuda.synchronize()
+        assert int(c.err.item()) == 16
+        # a plan made for another number of heads: nothing is written
+        c.err.zero_()
+        c.tabled.copy_(i32(c.table))
+        P.ops.prism_op_attention_paged_plan(c.cud, c.kvd, c.qd.shape[0], c.max_q, 8, 8, 128, BF16, 1, c.plan, c.err)
+        c.outd.fill_(3.0)
+        c.attend()
+        torch.cuda.synchronize()
+        assert int(c.err.item()) == 2 and (c.outd == 3).all()
+        # lengths beyond the table's row
+        c.err.zero_()
+        c.kvd.copy_(i32([50, 100000]))
+        c.make_plan()
+        c.attend()
+        torch.cuda.synchronize()
+        assert int(c.err.item()) == 16
+    # offsets that fall, a sequence longer than max_q_len, offsets beyond the rows of q, a negative length
+    for cu, kv in (([0, 5, 3], [9, 9]), ([0, 41, 41], [50, 9]), ([0, 1, 2000], [5, 5]), ([0, 1, 2], [5, -1])):
+        c.err.zero_()
+        c.cud.copy_(i32(cu))
+        c.kvd.copy_(i32(kv))
+        c.outd.fill_(3.0)
+        c.make_plan()
+        c.attend()
+        torch.cuda.synchronize()
+        assert int(c.err.item()) == 2 and (c.outd == 3).all()
+
+
+def test_attention_with_a_plan_for_longer_tables_and_no_workspace(P):
+    """Lengths that would be cut, a table too narrow for any cut and no workspace: reported, nothing outside is touched."""
+    for new in ([1], [40]):
+        c = Call(P, np.random.default_rng(22), new, [200], 16, 8, 128, BF16, 1, 16, need_ws=False)
+        c.kvd.copy_(i32([1 << 20]))
+        c.make_plan()
+        c.attend()
+        torch.cuda.synchronize()
+        assert int(c.err.item()) == 16
+
+
+def test_cache_beyond_32_bit_offsets(P):
+    """Pages 2^24 elements apart: the last ones start past 2^31 elements."""
+    stride, pages, hkv, dh, page = 1 << 24, 200, 2, 128, 16
+    arena = torch.empty(2, pages * stride, dtype=torch.bfloat16, device="cuda")
+    caches = [a.as_strided((pages, hkv, page, dh), (stride, page * dh, dh, 1)) for a in arena]
+    rng = np.random.default_rng(30)
+    for new in ([1], [30]):
+        c = Call(P, rng, new, [70], 4, 2, 128, BF16, 1, 16)
+        where = np.array([199, 0, 150, 131, 198])
+        x = draw(rng, BF16, 70, 8 * dh)
+        slots = np.repeat(where, 16)[:70] * 16 + np.arange(70) % 16
+        q = torch.empty(70, 4 * dh, dtype=torch.bfloat16, device="cuda")
+        P.ops.prism_op_qknorm_rope_paged(dev(x, BF16), BF16, i32(np.zeros(70)), i32(slots), 4, 0, None, None, 0.0, 1e4, q, *caches,
+                                         c.err)
+        c.k = np.zeros((pages, hkv, page, dh), np.float32)
+        c.v = np.zeros_like(c.k)
+        c.k[slots // 16, :, slots % 16] = x.reshape(70, 8, dh)[:, 4:6]
+        c.v[slots // 16, :, slots % 16] = x.reshape(70, 8, dh)[:, 6:]
+        c.table[0, :5] = where
+        c.tabled.copy_(i32(c.table))
+        c.kd, c.vd = caches
+        c.run()
+    c = Call(P, rng, [3], [70], 4, 2, 128, FP32, 1, 16)
+    arena = arena.view(torch.float32)
+    caches = [a.as_strided((pages, hkv, page, dh), (stride // 2, page * dh, dh, 1)) for a in arena]
+    k32, v32 = draw(rng, FP32, 5, hkv, page, dh), draw(rng, FP32, 5, hkv, page, dh)
+    c.k, c.v = np.zeros((pages, hkv, page, dh), np.float32), np.zeros((pages, hkv, page, dh), np.float32)
+    c.k[where], c.v[where] = k32, v32
+    for i, p in enumerate(where):
+        caches[0][p], caches[1][p] = dev(k32[i], FP32), dev(v32[i], FP32)
+    c.table[0, :5] = where
+    c.tabled.copy_(i32(c.table))
+    c.kd, c.vd = caches
+    c.run()
+
+
+def test_work_waits_for_another_streams_writes(P):
+    """Inputs written on a side stream, then used on the current one after an event: the operators start behind it."""
+    c = Call(P, np.random.default_rng(31), [40, 3], [500, 90], 16, 8, 128, BF16, 1, 16)
+    good = c.qd.clone()
+    c.qd.zero_()
+    side, ev = torch.cuda.Stream(), torch.cuda.Event()
+    big = torch.empty(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(10):
+            big.fill_(1.0)
+        c.qd.copy_(good)
+        ev.record()
+    c.make_plan()
+    torch.cuda.current_stream().wait_event(ev)
+    c.attend()
+    c.check()
+
+
+# ------------------------------------------------------------------------------------------------ together
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_a_request_over_the_cache(P, dtype):
+    """A request as a program would run it, two layers deep: a prompt is cached once, candidates' documents are appended behind
+    it, one probe drops some of them, the survivors get one more token each.  Every attention output is compared with dense
+    attention, in 64 bits, over everything the sequence has seen; the keys that dense attention uses are the cache's own
+    rows, which the rotation's test covers."""
+    rng = np.random.default_rng(40)
+    hq, hkv, dh, page, theta, layers = 4, 2, 64, 16, 1e4, 2
+    width, n, prompt = (hq + 2 * hkv) * dh, 9, 32
+    pool = 200
+    caches = [torch.zeros(pool, 2, hkv, page, dh, dtype=tdt(dtype), device="cuda") for _ in range(layers)]
+    gq, gk = dev(1 + 0.125 * rng.normal(size=dh).astype(np.float32), dtype), dev(1 + 0.125 * rng.normal(size=dh).astype(np.float32), dtype)
+    err = err_word()
+    free, n_free = i32(rng.permutation(pool)), i32([pool])
+    max_pages = 16
+    used = {}                                          # sequence -> its qkv rows per layer, oldest first
+
+    def step(kv, table, lens, ids):
+        """Append `lens` tokens to every sequence and run the layers.  ids: which candidate each row of the table is."""
+        m, total = len(lens), int(np.sum(lens)) + 3    # three padding rows
+        cu, pos, slot = i32(np.zeros(m + 1)), i32(np.zeros(total)), i32(np.zeros(total))
+        P.ops.prism_op_page_append(i32(lens), kv, kv, page, pool, table, free, n_free, n_free, cu, pos, slot, err)
+        max_q = int(max(lens))
+        pb, wb = P.ops.prism_op_attention_paged_bytes(m, total, max_q, hq, hkv, dh, dtype)
+        plan, ws = torch.empty(pb, dtype=torch.uint8, device="cuda"), torch.empty(wb, dtype=torch.uint8, device="cuda")
+        P.ops.prism_op_attention_paged_plan(cu, kv, total, max_q, hq, hkv, dh, dtype, 1, plan, err)
+        for layer in range(layers):
+            x = draw(rng, dtype, total, width)
+            q = torch.empty(total, hq * dh, dtype=tdt(dtype), device="cuda")
+            out = torch.full((total, hq * dh), 3.0, dtype=tdt(dtype), device="cuda")
+            k, v = caches[layer][:, 0], caches[layer][:, 1]
+            P.ops.prism_op_qknorm_rope_paged(dev(x, dtype), dtype, pos, slot, hq, 1, gq, gk, 1e-6, theta, q, k, v, err)
+            P.ops.prism_op_attention_paged(q, k, v, table, plan, m, max_q, hq, dtype, out, ws, err)
+            torch.cuda.synchronize()
+            assert int(err.item()) == 0
+            c = np.concatenate([[0], np.cumsum(lens)])
+            for i, who in enumerate(ids):
+                used.setdefault((layer, who), []).append(x[c[i]:c[i + 1]])
+                rows = np.concatenate(used.get((layer, "prompt"), [])[:0 if who == "prompt" else 1] + used[(layer, who)])
+                xs = rows.astype(np.float64).reshape(len(rows), hq + 2 * hkv, dh)
+                p = np.arange(len(rows))
+                assert int(kv[i].item()) == len(rows)
+                want_k, size_k = norm_rope(xs[:, hq:hq + hkv], p, host(gk), 1e-6, theta)
+                # what the cache holds for this sequence: the rotated keys to one rounding, the values exactly
+                ids_ = table[i, :pages_of(len(rows), page)].long()
+                have = [host(t[ids_]).transpose(0, 2, 1, 3).reshape(-1, hkv, dh)[:len(rows)] for t in (k, v)]
+                half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+                assert (np.abs(have[0] - want_k) <= half * np.abs(want_k) + (dh / 2 + 17) * 2.0 ** -24 * size_k).all()
+                assert np.array_equal(have[1], xs[:, hq + hkv:])
+                cache = [np.ascontiguousarray(h.transpose(1, 0, 2))[None] for h in have]     # one page of len(rows) tokens
+                o, avg, size = attention(host(q[c[i]:c[i + 1]]).reshape(-1, hq, dh), *cache, np.zeros((1, 1), int),
+                                         np.array([0, lens[i]]), np.array([len(rows)]), 1)
+                tol = attention_tolerance(o, avg, size, dh, len(rows), dtype == BF16)
+                assert (np.abs(host(out[c[i]:c[i + 1]]).reshape(-1, hq, dh) - o) <= tol).all()
+            assert (out[-3:] == 3).all()
+
+    # the prompt, as a sequence of its own
+    t0, kv0 = i32(np.full((1, max_pages), -1)), i32([0])
+    step(kv0, t0, [prompt], ["prompt"])
+    # every candidate starts as the prompt's two pages
+    table = t0.repeat(n, 1)
+    kv = kv0.repeat(n)
+    step(kv, table, rng.integers(1, 60, size=n).tolist(), list(range(n)))
+    free_before = int(n_free.item())
+    keep = np.array([1, 3, 4, 8])
+    table2 = torch.empty_like(table)
+    pages_before = [pages_of(int(x), page) for x in kv.cpu().numpy()]
+    P.ops.prism_op_page_release(i32(keep), kv, kv, page, pool, prompt // page, table, table2, free, n_free, n_free, err)
+    torch.cuda.synchronize()
+    assert int(n_free.item()) - free_before == sum(pages_before[s] - 2 for s in range(n) if s not in keep)
+    for _ in range(3):
+        step(kv[:4], table2[:4], [1] * 4, keep.tolist())
+    step(kv[:4], table2[:4], [20, 1, 7, 33], keep.tolist())

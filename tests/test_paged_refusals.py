@@ -1,0 +1,156 @@
+"""CPU-only: what the paged-cache entry points refuse, before any device is touched (pointers are never followed)."""
+import ctypes as C
+
+import pytest
+
+import paper_2510_15620_b200 as P
+from paper_2510_15620_b200 import ops
+
+OK, INVALID, LIMIT, UNSUPPORTED = 0, -1, -2, -8
+FP32, BF16 = 0, 1
+
+
+@pytest.fixture(scope="module")
+def L():
+    return ops._L()
+
+
+@pytest.fixture(scope="module")
+def buf():
+    raw = (C.c_uint8 * 65536)()
+    base = (C.addressof(raw) + 255) & ~255
+    return raw, base            # the array has to outlive the calls
+
+
+def cache(base, **kw):
+    d = dict(k=base, v=base, page_stride=2 * 16 * 64, num_pages=8, page_size=16, n_kv_heads=2, head_dim=64, dtype=BF16)
+    d.update(kw)
+    return ops._KvCache(**d)
+
+
+def append(L, p, **kw):
+    d = dict(len_new=p, kv_in=p, kv_out=p, n=4, page=16, num_pages=8, max_pages=4, stride=4, table=p, free=p, nf_in=p, nf_out=p,
+             total=8, cu=p, pos=p, slot=p, err=p)
+    d.update(kw)
+    return L.prism_op_page_append(*d.values(), None)
+
+
+def release(L, p, **kw):
+    d = dict(keep=p, n_new=2, kv_in=p, kv_out=p, n=4, page=16, num_pages=8, shared=0, max_pages=4, s_in=4, t_in=p, s_out=4,
+             t_out=p + 4096, free=p, nf_in=p, nf_out=p, err=p)
+    d.update(kw)
+    return L.prism_op_page_release(*d.values(), None)
+
+
+def test_append_refuses(L, buf):
+    p = buf[1]
+    for kw in (dict(n=-1), dict(total=-1), dict(page=0), dict(page=8), dict(page=24), dict(page=512), dict(num_pages=-1),
+               dict(max_pages=-1), dict(stride=3), dict(num_pages=1 << 27), dict(max_pages=1 << 27, stride=1 << 27),
+               dict(len_new=None), dict(kv_in=None), dict(kv_out=None), dict(table=None), dict(free=None), dict(nf_in=None),
+               dict(nf_out=None), dict(cu=None), dict(pos=None), dict(slot=None), dict(err=None)):
+        assert append(L, p, **kw) == INVALID, kw
+    assert append(L, p, n=4097) == LIMIT
+
+
+def test_release_refuses(L, buf):
+    p = buf[1]
+    for kw in (dict(n=-1), dict(n_new=-1), dict(n_new=5), dict(shared=-1), dict(page=20), dict(s_in=3), dict(s_out=3),
+               dict(t_out=p), dict(t_out=p + 60), dict(t_in=p + 4096 + 16), dict(keep=None), dict(kv_in=None), dict(kv_out=None),
+               dict(t_in=None), dict(t_out=None), dict(free=None), dict(nf_in=None), dict(nf_out=None), dict(err=None)):
+        assert release(L, p, **kw) == INVALID, kw
+    assert release(L, p, n=4097, n_new=0, t_out=p + (1 << 24)) == LIMIT
+
+
+def rope(L, p, c=None, **kw):
+    c = cache(p) if c is None else c            # 0: no cache at all
+    d = dict(qkv=p, s_in=8 * 64, pos=p, slot=p, rows=4, hq=4, norm=1, g_q=p, g_k=p, eps=1e-6, theta=1e4, q=p, s_out=4 * 64,
+             c=C.byref(c) if c != 0 else None, err=p)
+    d.update(kw)
+    return L.prism_op_qknorm_rope_paged(*d.values(), None)
+
+
+def test_norm_and_rotation_refuse(L, buf):
+    p = buf[1]
+    assert rope(L, p, rows=0) == OK                      # nothing to do: nothing is launched
+    for kw in (dict(rows=-1), dict(hq=0), dict(theta=0.0), dict(theta=float("nan")), dict(eps=-1.0), dict(s_in=8 * 64 - 8),
+               dict(s_in=8 * 64 + 1), dict(s_out=4 * 64 - 8), dict(s_out=4 * 64 + 4), dict(qkv=p + 2), dict(q=p + 8),
+               dict(g_q=p + 4), dict(g_q=None), dict(g_k=None), dict(qkv=None), dict(pos=None), dict(slot=None), dict(q=None),
+               dict(err=None), dict(c=0)):
+        assert rope(L, p, **kw) == INVALID, kw
+    check_caches(lambda c: rope(L, p, c=c, s_in=1 << 20, s_out=1 << 20), p)
+
+
+def check_caches(call, p):
+    for kw in (dict(k=None), dict(v=None), dict(k=p + 8), dict(num_pages=0), dict(num_pages=1 << 27), dict(page_size=12),
+               dict(page_size=48), dict(n_kv_heads=0), dict(dtype=2), dict(page_stride=2 * 16 * 64 - 8),
+               dict(page_stride=2 * 16 * 64 + 4), dict(page_stride=1 << 39)):
+        assert call(cache(p, **kw)) == INVALID, kw
+    for kw in (dict(head_dim=8), dict(head_dim=72, page_stride=1 << 20), dict(head_dim=272, page_stride=1 << 20)):
+        assert call(cache(p, **kw)) == UNSUPPORTED, kw
+
+
+def sizes(L, **kw):
+    d = dict(n=4, total=8, max_q=2, hq=4, hkv=2, dh=64, dtype=BF16, impl=0)
+    d.update(kw)
+    a, b = C.c_int64(), C.c_int64()
+    rc = L.prism_op_attention_paged_bytes(*d.values(), C.byref(a), C.byref(b))
+    return rc, a.value, b.value
+
+
+def test_attention_sizes(L):
+    rc, plan, ws = sizes(L)
+    assert rc == OK and plan > 0 and ws > 0
+    for kw in (dict(n=-1), dict(total=-1), dict(max_q=-1), dict(hq=0), dict(hkv=0), dict(hq=5), dict(dtype=3)):
+        assert sizes(L, **kw)[0] == INVALID, kw
+    for kw in (dict(impl=2), dict(impl=3), dict(dh=20), dict(dh=512), dict(hq=258, hkv=2), dict(hq=130, hkv=2, dtype=FP32),
+               dict(hq=130, hkv=2, impl=1)):
+        assert sizes(L, **kw)[0] == UNSUPPORTED, kw
+    assert sizes(L, n=4097)[0] == LIMIT
+    # few tokens of a group wider than a tile of rows, and no tokens at all
+    assert sizes(L, hq=40, hkv=2, max_q=1)[0] == OK
+    assert sizes(L, hq=40, hkv=2, max_q=0, total=0)[0] == OK
+    assert sizes(L, n=0, total=0)[0] == OK
+    assert ops.prism_op_attention_paged_bytes(4, 8, 2, 4, 2, 64, BF16) == (plan, ws)
+
+
+def plan(L, p, **kw):
+    d = dict(cu=p, kv=p, n=4, total=8, max_q=2, hq=4, hkv=2, dh=64, dtype=BF16, causal=1, impl=0, plan=p, bytes=1 << 30, err=p)
+    d.update(kw)
+    return L.prism_op_attention_paged_plan(*d.values(), None)
+
+
+def attn(L, p, c=None, **kw):
+    c = cache(p) if c is None else c
+    d = dict(q=p, s_q=256, c=C.byref(c) if c != 0 else None, table=p, stride=32, max_pages=32, plan=p, plan_bytes=1 << 30, n=4, total=8, max_q=2, hq=4,
+             impl=0, out=p, s_out=256, ws=p, ws_bytes=1 << 40, err=p)
+    d.update(kw)
+    return L.prism_op_attention_paged(*d.values(), None)
+
+
+def test_attention_refuses(L, buf):
+    p = buf[1]
+    need_plan, need_ws = sizes(L)[1:]
+    for kw in (dict(cu=None), dict(kv=None), dict(plan=None), dict(err=None), dict(plan=p + 8), dict(bytes=need_plan - 1), dict(n=-1),
+               dict(hq=3)):
+        assert plan(L, p, **kw) == INVALID, kw
+    assert plan(L, p, n=4097) == LIMIT
+    assert plan(L, p, impl=2) == UNSUPPORTED
+    for kw in (dict(n=0), dict(total=0), dict(max_q=0)):
+        assert attn(L, p, **kw) == OK, kw                # nothing to do: nothing is launched
+    for kw in (dict(q=None), dict(out=None), dict(table=None), dict(plan=None), dict(err=None), dict(ws=None), dict(c=0),
+               dict(q=p + 8), dict(out=p + 4), dict(plan=p + 4), dict(ws=p + 8), dict(plan_bytes=need_plan - 1),
+               dict(ws_bytes=need_ws - 1), dict(s_q=248), dict(s_q=260), dict(s_out=252), dict(stride=31), dict(max_pages=-1),
+               dict(max_pages=1 << 27, stride=1 << 27), dict(hq=5), dict(n=-1)):
+        assert attn(L, p, **kw) == INVALID, kw
+    assert attn(L, p, impl=3) == UNSUPPORTED
+    check_caches(lambda c: attn(L, p, c=c), p)
+
+
+def test_host_tensors_are_refused():
+    import torch
+    i = torch.zeros(8, dtype=torch.int32)
+    with pytest.raises(P.PrismError) as e:
+        ops.prism_op_page_append(i, i, i, 16, 8, i.view(2, 4), i, i, i, i, i, i, i)
+    assert e.value.status == INVALID
+    with pytest.raises(P.PrismError):
+        ops.prism_op_attention_paged_plan(i, i[:4], 8, 2, 4, 2, 64, BF16, 1, i, i)
