@@ -11,11 +11,14 @@ namespace prism {
 namespace {
 
 constexpr int kPlanThreads = 1024;
+constexpr int kSearch = 1024;
 
 // ------------------------------------------------------------------------------------------------ work list
 // One block.  Tiles of s.tokens tokens; a tile whose keys are more than `piece` is cut into equal pieces so that few long
-// sequences still occupy every SM.  The piece length is the launch's total (keys x heads) over s.target, hence the bounds
-// of paged_plan_bounds.  Tiles are listed from the last to the first: under causal attention a sequence's last tile has the
+// sequences still occupy every SM.  Up to kSearch tiles, 32 warps weigh 32 piece lengths against each other (no cut, the
+// longest tile over 2, 3, ... 32): waves of blocks times a mean piece, plus what the longest piece exceeds it by.  Beyond that
+// the SMs are busy anyway and only tiles far longer than the others are cut.  No piece is shorter than the launch's
+// total (keys x heads) over s.target, hence the bounds of paged_plan_bounds.  Tiles are listed from the last to the first: under causal attention a sequence's last tile has the
 // most keys, and the launch should end on light ones.
 struct Sums {
   long long a, b, c;
@@ -55,6 +58,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restri
                                                              PagedPlanShape sh, PagedPlanBounds bound, void* plan, int* err) {
   extern __shared__ int s_tile[];  // [n + 1] first tile of each sequence
   __shared__ Sums warp_tot[33];
+  __shared__ int s_keys[kSearch], s_longest[32], s_len[32];
+  __shared__ float s_cost[32];
   const int tid = threadIdx.x;
   PagedPlanHeader* hd = static_cast<PagedPlanHeader*>(plan);
   PagedItem* items = reinterpret_cast<PagedItem*>(hd + 1);
@@ -96,10 +101,46 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restri
     return r;
   };
   Sums w{0, 0, 0};
-  for (int t = tid; t < n_tiles; t += kPlanThreads) w.a += tile_at(t).keys;
+  int longest = 0;
+  for (int t = tid; t < n_tiles; t += kPlanThreads) {
+    const int keys = tile_at(t).keys;
+    w.a += keys;
+    longest = max(longest, keys);
+    if (t < kSearch) s_keys[t] = keys;
+  }
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  if ((tid & 31) == 0) s_longest[tid >> 5] = longest;
   plan_scan(w, warp_tot, tot);
-  long long piece = (tot.a * hkv + sh.target - 1) / sh.target;
+  const long long all_keys = tot.a;
+  long long piece = (all_keys * hkv + sh.target - 1) / sh.target;
   piece = piece < sh.min_piece ? sh.min_piece : piece;
+  if (n_tiles <= kSearch) {
+    longest = __reduce_max_sync(0xffffffffu, s_longest[tid & 31]);
+    const int j = tid >> 5, lane = tid & 31;
+    unsigned len = j == 0 ? 0x7fffffffu : (unsigned)((longest + j) / (j + 1) + sh.piece_unit - 1) / sh.piece_unit * sh.piece_unit;
+    if (len < piece) len = (unsigned)min(piece, 0x7fffffffll);
+    unsigned items_n = 0, parts_n = 0;
+    for (int t = lane; t < n_tiles; t += 32) {
+      const unsigned k = s_keys[t], c = max(1u, (k + len - 1) / len);
+      items_n += c;
+      parts_n += c > 1 ? c : 0;
+    }
+    items_n = __reduce_add_sync(0xffffffffu, items_n);
+    parts_n = __reduce_add_sync(0xffffffffu, parts_n);
+    if (lane == 0) {
+      const float n_work = (float)items_n * hkv, mean = items_n ? (float)all_keys / items_n : 0.f;
+      const float most = (float)min(len, (unsigned)longest);
+      const float key = fmaxf(sh.ns_key, sh.ns_key_block * fminf(n_work, (float)sh.slots));
+      s_cost[j] = ceilf(n_work / sh.slots) * (mean * key + sh.ns_item) + fmaxf(most - mean, 0.f) * key +
+                  (parts_n ? parts_n * hkv * sh.ns_part / fminf(n_work, (float)sh.slots) + sh.ns_join : 0.f);
+      s_len[j] = (int)len;
+    }
+    __syncthreads();
+    float best = s_cost[0];
+    piece = s_len[0];
+    for (int i = 1; i < 32; ++i)
+      if (s_cost[i] < best) best = s_cost[i], piece = s_len[i];
+  }
   int base = 0, base_part = 0, base_join = 0;
   for (int t0 = 0; t0 < n_tiles; t0 += kPlanThreads) {
     const int i = t0 + tid, t = n_tiles - 1 - i;
@@ -149,70 +190,86 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restri
 
 // ------------------------------------------------------------------------------------------------ joining pieces
 // out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i, M = max_i m_i, over the pieces in which the row sees a key.
-// Eight lanes share a (row, 16 columns): each takes every eighth piece, and a butterfly adds them in a fixed order.
-template <typename T>
+// S lanes share a (row, 16 columns): each takes every S-th piece, and a butterfly adds them in a fixed order.  Eight where
+// there are few rows (and often many pieces); one where rows are many, so that a warp's lanes are 32 neighbouring rows.
+template <typename T, int S>
 __global__ void __launch_bounds__(256) k_paged_join(PagedPlanHeader want, const PagedPlanHeader* __restrict__ hd,
                                                     long long items_cap, const float* __restrict__ ws, T* __restrict__ out,
-                                                    long long out_stride) {
+                                                    long long out_stride, int live_rows) {
   pdl_sync();
   if (hd->kind != want.kind || hd->hq != want.hq || hd->hkv != want.hkv || hd->dh != want.dh || hd->total_q != want.total_q ||
       hd->n_seq != want.n_seq || hd->max_q != want.max_q)
     return;  // the attention kernel has reported it
   const PagedJoin* joins = reinterpret_cast<const PagedJoin*>(reinterpret_cast<const PagedItem*>(hd + 1) + items_cap);
   const int rows = want.rows, dh = want.dh, hkv = want.hkv, group = want.hq / hkv, chunks = dh / 16;
-  const long long per_join = (long long)hkv * chunks * rows, total = per_join * hd->n_joins;
+  const int per_join = hkv * chunks * live_rows;
+  const long long total = (long long)per_join * hd->n_joins;
   const long long part_floats = paged_part_floats(rows, dh);
-  const int sub = threadIdx.x & 7;
-  for (long long u = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 3; u < total;
-       u += ((long long)gridDim.x * blockDim.x) >> 3) {
-    const PagedJoin jn = joins[u / per_join];
-    const int rem = (int)(u % per_join), r = rem % rows, ch = rem / rows % chunks, h = rem / rows / chunks;
-    const int tok = r / group;
-    if (tok >= jn.n_tok) continue;  // the eight lanes of a row agree
-    const unsigned lanes = 0xffu << (threadIdx.x & 24);
+  const int sub = threadIdx.x & (S - 1);
+  const unsigned lanes = S == 1 ? 0u : ((1u << S) - 1) << (threadIdx.x & (32 - S));
+  for (long long u = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / S; u < total;
+       u += ((long long)gridDim.x * blockDim.x) / S) {
+    const int which = (int)(u / per_join), rem = (int)(u % per_join), r = rem % live_rows, ch = rem / live_rows % chunks;
+    const int h = rem / live_rows / chunks, tok = r / group;
+    const PagedJoin jn = joins[which];
+    if (tok >= jn.n_tok) continue;  // the lanes of a row agree
     const int pos = jn.pos0 + tok;
     // pieces in which this row sees a key
     int n_parts = jn.n_parts;
     if (jn.causal) n_parts = pos < 0 ? 0 : min(n_parts, pos / jn.piece + 1);
     const float* base = ws + ((long long)jn.part0 * hkv + h) * part_floats;
+    const float* ml = base + (long long)rows * dh + 2 * r;
+    const float* po = base + ((long long)ch * 4 * rows + r) * 4;
     const long long step = (long long)hkv * part_floats;
     float m = -INFINITY;
-    for (int i = sub; i < n_parts; i += 8) m = fmaxf(m, base[i * step + (long long)rows * dh + 2 * r]);
+#pragma unroll 4
+    for (int i = sub; i < n_parts; i += S) m = fmaxf(m, ml[i * step]);
 #pragma unroll
-    for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, d));
+    for (int d = S >> 1; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, d));
     const float ref = m == -INFINITY ? 0.f : m;
     float l = 0.f, o[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[e] = 0.f;
-    for (int i = sub; i < n_parts; i += 8) {
-      const float* p = base + i * step;
-      const float2 ml = *reinterpret_cast<const float2*>(p + (long long)rows * dh + 2 * r);
-      const float w = exp2f(ml.x - ref);
-      l += w * ml.y;
+#pragma unroll 2
+    for (int i = sub; i < n_parts; i += S) {
+      const float2 x = *reinterpret_cast<const float2*>(ml + i * step);
+      const float w = exp2f(x.x - ref);
+      l += w * x.y;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float4 v = *reinterpret_cast<const float4*>(p + ((long long)(ch * 4 + e) * rows + r) * 4);
+        const float4 v = *reinterpret_cast<const float4*>(po + i * step + (long long)e * rows * 4);
         o[4 * e] += w * v.x, o[4 * e + 1] += w * v.y, o[4 * e + 2] += w * v.z, o[4 * e + 3] += w * v.w;
       }
     }
 #pragma unroll
-    for (int d = 4; d > 0; d >>= 1) {
+    for (int d = S >> 1; d > 0; d >>= 1) {
       l += __shfl_xor_sync(lanes, l, d);
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[e] += __shfl_xor_sync(lanes, o[e], d);
     }
-    const float inv = n_parts > 0 ? 1.f / l : 0.f;
-    T* dst = out + (jn.row0 + tok) * out_stride + (long long)(h * group + r % group) * dh + ch * 16 + sub * 2;
-    float v0 = 0.f, v1 = 0.f;
+    const float inv = 1.f / l;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e == sub) v0 = o[2 * e], v1 = o[2 * e + 1];
-    v0 = n_parts > 0 ? v0 * inv : 0.f;
-    v1 = n_parts > 0 ? v1 * inv : 0.f;
-    if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(v0, v1);
-    else
-      *reinterpret_cast<float2*>(dst) = make_float2(v0, v1);
+    for (int e = 0; e < 16; ++e) o[e] = n_parts > 0 ? o[e] * inv : 0.f;
+    T* dst = out + (jn.row0 + tok) * out_stride + (long long)(h * group + r % group) * dh + ch * 16;
+    constexpr int N = 16 / S;  // columns this lane stores
+#pragma unroll
+    for (int k = 0; k < S; ++k)
+      if (k == sub) {
+        if constexpr (sizeof(T) == 2) {
+          __align__(16) __nv_bfloat162 b[N / 2];
+#pragma unroll
+          for (int e = 0; e < N; e += 2) b[e / 2] = __floats2bfloat162_rn(o[k * N + e], o[k * N + e + 1]);
+          if constexpr (N == 16) {
+            reinterpret_cast<uint4*>(dst)[0] = reinterpret_cast<uint4*>(b)[0];
+            reinterpret_cast<uint4*>(dst)[1] = reinterpret_cast<uint4*>(b)[1];
+          } else {
+            *reinterpret_cast<__nv_bfloat162*>(dst + k * N) = b[0];
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(dst + k * N + e) = make_float2(o[k * N + e], o[k * N + e + 1]);
+        }
+      }
   }
 }
 
@@ -400,18 +457,23 @@ bool paged_plan_shape(int max_q, int hq, int hkv, int dh, int dtype, int impl, P
   if (max_q < 1) max_q = 1;
   s->group = g;
   s->piece_unit = 128;
+  s->target = 148 * 8;
   const bool few = (long long)max_q * g <= 16;
   if (dtype == 1 && impl == 0 && (dh == 64 || dh == 128) && g <= 128) {
     if (few) {
-      // tokens: the whole sequence's new rows fit one 16-row tile
-      s->kind = kPagedTokens, s->rows = 16, s->tokens = 16 / g, s->min_piece = 256, s->target = 148 * 4;
+      // the whole sequence's new rows fit one 16-row tile; two blocks per SM, together at the memory's rate (6.4 TB/s)
+      s->kind = kPagedTokens, s->rows = 16, s->tokens = 16 / g, s->min_piece = 256, s->slots = 148 * 2;
+      s->ns_key = 4.f * dh / 100.f, s->ns_key_block = 4.f * dh / 6400.f, s->ns_item = 1500.f, s->ns_part = 200.f, s->ns_join = 2500.f;
     } else {
-      s->kind = kPagedTiles, s->rows = 256, s->tokens = 2 * (128 / g), s->min_piece = 1024, s->target = 148 * 4;
+      // bound by each SM's own tensor core and softmax; a partial result is 133 KB written and read
+      s->kind = kPagedTiles, s->rows = 256, s->tokens = 2 * (128 / g), s->min_piece = 1024, s->slots = 148;
+      s->ns_key = 20.f, s->ns_key_block = 0.f, s->ns_item = 3000.f, s->ns_part = 6000.f, s->ns_join = 4000.f;
     }
     return true;
   }
   if (g > 64) return false;
-  s->kind = kPagedSimt, s->rows = few ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 256, s->target = 148 * 4;
+  s->kind = kPagedSimt, s->rows = few ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 256, s->slots = 148 * 2;
+  s->ns_key = few ? 10.f : 40.f, s->ns_key_block = 0.f, s->ns_item = 2000.f, s->ns_part = 1000.f, s->ns_join = 2500.f;
   return true;
 }
 
@@ -428,7 +490,9 @@ cudaError_t launch_paged_join(const PagedAttnArgs& a, const PagedPlanShape& s, i
   PagedPlanHeader want{};
   want.kind = s.kind, want.hq = a.hq, want.hkv = a.c.hkv, want.dh = a.c.dh, want.total_q = a.total_q, want.n_seq = a.n_seq;
   want.max_q = a.max_q, want.rows = s.rows;
-  const long long threads = (long long)max_joins * a.c.hkv * (a.c.dh / 16) * s.rows * 8;
+  const int tokens = a.max_q < s.tokens ? a.max_q : s.tokens, live_rows = tokens * s.group;
+  const int lanes = s.rows == 16 ? 8 : 1;
+  const long long threads = (long long)max_joins * a.c.hkv * (a.c.dh / 16) * live_rows * lanes;
   long long grid = (threads + 255) / 256;
   if (grid > 148 * 8) grid = 148 * 8;
   cudaLaunchConfig_t cfg = {};
@@ -442,10 +506,11 @@ cudaError_t launch_paged_join(const PagedAttnArgs& a, const PagedPlanShape& s, i
   cfg.attrs = attr;
   cfg.numAttrs = pdl_enabled() ? 1 : 0;
   const PagedPlanHeader* hd = static_cast<const PagedPlanHeader*>(a.plan);
-  if (a.c.dtype == 1)
-    return cudaLaunchKernelEx(&cfg, k_paged_join<__nv_bfloat16>, want, hd, b.items, (const float*)a.ws,
-                              (__nv_bfloat16*)a.out, a.out_stride);
-  return cudaLaunchKernelEx(&cfg, k_paged_join<float>, want, hd, b.items, (const float*)a.ws, (float*)a.out, a.out_stride);
+#define PRISM_JOIN(T, S) \
+  cudaLaunchKernelEx(&cfg, k_paged_join<T, S>, want, hd, b.items, (const float*)a.ws, (T*)a.out, a.out_stride, live_rows)
+  if (a.c.dtype == 1) return lanes == 8 ? PRISM_JOIN(__nv_bfloat16, 8) : PRISM_JOIN(__nv_bfloat16, 1);
+  return lanes == 8 ? PRISM_JOIN(float, 8) : PRISM_JOIN(float, 1);
+#undef PRISM_JOIN
 }
 
 cudaError_t launch_paged_simt(const PagedAttnArgs& a, const PagedPlanShape& s, int grid, cudaStream_t st) {

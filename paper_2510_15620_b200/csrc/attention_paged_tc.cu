@@ -10,16 +10,26 @@
 // One persistent CTA per SM.  Units are handed out by the hardware's work distributor: the grid has one CTA per possible
 // unit, and a running CTA takes over the next one that has not started (clusterlaunchcontrol.try_cancel), so there is no
 // counter in memory that launches could share.  The request is made when a unit starts and answered long before it ends.
-// Warp-specialised, 576 threads:
+// Warp-specialised, 320 threads:
 //   warp 0      producer: units, Q tiles, and key/value tiles page by page: every lane owns one (page, 64-column half) box of a
 //               tile, so a tile of eight 16-token pages costs one instruction per lane; page numbers are read a tile ahead
 //   warp 1      the only MMA issuer: S_x = Q_x K_j^T and O_x += P_x V_j (P from tensor memory, V as MN-major operand), in
-//               the order PV_A(g) S_A(g+1) PV_B(g) S_B(g+1)
-//   warps 2..9  softmax of A, warps 10..17 of B: two threads per row, exponentials against a per-row reference that starts
-//               as the row's score on the piece's first key (a row that sees any key of a piece sees that one) and moves, by
-//               whole powers of two, only when a row sum threatens fp32 range
+//               the order PV_A(g) S_A(g+1) PV_B(g) S_B(g+1), each P V in two halves of 64 keys
+//   warps 2..5  softmax of A, warps 6..9 of B: one thread per row (no exchange between threads: the row's reference and sum
+//               are its own), exponentials against a reference that starts as the row's score on the piece's first key (a row
+//               that sees any key of a piece sees that one) and moves, by whole powers of two, only when a sum threatens
+//               fp32 range
 // Tensor memory: S_A, S_B, O_A, O_B.  P_x(g) overlies S_x(g).  Rows that no token owns are not computed; a warp without any
 // live row only keeps the barriers' phases.
+//
+// What bounds it: the chain softmax -> P V -> next scores of each tile (2430 + 1330 cycles a block, clock64), which the other
+// tile covers to two thirds; tensor core and special-function unit are 55-60 % busy.  Measured steps (us; 2368 tokens behind
+// 16 k / 1024 behind 64 k / 100 documents of 320 behind 512): two threads per row that meet once a block 625 / 1066 / 284; one
+// thread per row, P V in halves 618 / 1093 / 279; MMAs issued by an elected thread instead of lane 0 (38 instead of 60 issue
+// cycles an instruction, which beside eight softmax warps decides who waits) 611 / 1074 / 255; the issuing warp in step
+// 608 / 1070 / 250; exponentials shared with the FMA pipe 568 / 1039 / 250.  Tried and not kept: two threads per row with one
+// deciding the reference for both 650 / 1120 / 286; whole rows in 208 registers (register reallocation) 638 / 1107 / 261;
+// scores double-buffered in blocks of 64 keys 614 / 1103 / 250; suspended instead of polled waits 675 / 1151 / 264.
 // Values behind the last key of a piece (stale rows of the last page) are cleared in shared memory before the second
 // product, so that nothing a page happens to hold meets a zero probability.
 // Rounding: probabilities become bf16 for the second product; sums, references and outputs stay fp32 until the one
@@ -37,14 +47,14 @@ using namespace tc;
 constexpr int BM = 128, BN = 128;
 constexpr int NK = 2, NV = 2;
 constexpr int kStageBytes = 32 * 64;  // per softmax warp: 32 rows x 32 bf16 of output on their way to global memory
-constexpr int kBarBytes = 640;
+constexpr int kBarBytes = 512;
 __host__ __device__ constexpr int tile_bytes(int dh) { return 128 * dh * 2; }
 __host__ __device__ constexpr int smem_bytes(int dh) {
-  return (2 + NK + NV) * tile_bytes(dh) + 16 * kStageBytes + 1024 /*alignment slack*/ + kBarBytes;
+  return (2 + NK + NV) * tile_bytes(dh) + 8 * kStageBytes + 1024 /*alignment slack*/ + kBarBytes;
 }
 static_assert(smem_bytes(128) <= 232448, "exceeds the shared memory one CTA may have");
 constexpr float kBigSum = 1.2089258e24f;  // 2^80: row sums of one block beyond this move the reference
-constexpr int kThreads = 576;
+constexpr int kThreads = 320;  // producer, MMA issuer, 2 x 4 softmax warps
 constexpr int kTmemCols = 512;
 constexpr int NI = 4;  // depth of the ring of published units
 
@@ -53,8 +63,65 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void tmem_ld1(uint32_t taddr, uint32_t& v) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(v) : "r"(taddr));
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+// The wait names the loaded registers, so that nothing that uses them can move in front of it.
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                 "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+// 2^(s * scale - ms) of 32 scores as 16 packed bf16 pairs (key 2 e in the low half), and their sum.
+// The special-function unit gives an SM 16 exponentials a clock, i.e. a 128 x 128 block of scores takes as long as its two
+// products; kOnFma of the 16 pairs are therefore formed on the FMA pipe: x = n + f, n = round(x) (adding 1.5 * 2^23 leaves n in
+// the low bits), 2^f by the degree-5 minimax polynomial on [-1/2, 1/2] (relative error 2^-23.6, as good as ex2.approx), n added
+// to the exponent field.  x is clamped to [-125, 126]: a masked score comes out as 2^-125 instead of 0 beside a sum of at least
+// 1, and one beyond fp32 range is still seen by the range check.
+// Measured (2368 tokens behind 16 k / 1024 behind 64 k, 32 query heads): none 607 / 1070 us, 2 pairs 572 / 1041, 3 568 / 1039,
+// 4 575 / 1043; short sequences indifferent.
+constexpr int kOnFma = 3;
+__device__ __forceinline__ void exp_chunk(const uint32_t* s, uint64_t sc2, float ms, uint32_t* pk, float& sum) {
+  const uint64_t nm2 = f2_pack(-ms, -ms);
+  const float kMagic = 12582912.f;
+  uint64_t acc[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const uint64_t xv = f2_fma(f2_pack(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), sc2, nm2);
+    float x0, x1, p0, p1;
+    f2_unpack(xv, x0, x1);
+    if ((e * kOnFma) / 16 != ((e + 1) * kOnFma) / 16) {
+      const uint64_t xc = f2_pack(fminf(fmaxf(x0, -125.f), 126.f), fminf(fmaxf(x1, -125.f), 126.f));
+      const uint64_t t = f2_add(xc, f2_pack(kMagic, kMagic));
+      const uint64_t f = f2_fma(f2_add(t, f2_pack(-kMagic, -kMagic)), f2_pack(-1.f, -1.f), xc);
+      uint64_t p = f2_fma(f2_pack(0.0013277939f, 0.0013277939f), f, f2_pack(0.009675758f, 0.009675758f));
+      p = f2_fma(p, f, f2_pack(0.0555071f, 0.0555071f));
+      p = f2_fma(p, f, f2_pack(0.24022114f, 0.24022114f));
+      p = f2_fma(p, f, f2_pack(0.69314694f, 0.69314694f));
+      p = f2_fma(p, f, f2_pack(1.0000001f, 1.0000001f));
+      float q0, q1, t0, t1;
+      f2_unpack(p, q0, q1);
+      f2_unpack(t, t0, t1);
+      p0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
+      p1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
+    } else {
+      p0 = ex2(x0), p1 = ex2(x1);
+    }
+    acc[e & 1] = f2_add(acc[e & 1], f2_pack(p0, p1));
+    pk[e] = pack_bf16(p0, p1);
+  }
+  float lo, hi;
+  f2_unpack(f2_add(acc[0], acc[1]), lo, hi);
+  sum = lo + hi;
 }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
   asm volatile(
@@ -89,6 +156,12 @@ __device__ __forceinline__ int answered_unit(uint32_t src) {
   return got ? (int)x : -1;
 }
 
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+
 struct Unit {
   int n_blocks;  // 0: no more units
   int row0, n_tok, pos0, k0, k1, part, h;
@@ -100,13 +173,12 @@ struct UnitReader {
   __device__ __forceinline__ void init(Unit* ring_, uint32_t b_full_, uint32_t b_empty_) {
     ring = ring_, b_full = b_full_, b_empty = b_empty_, n = 0, n_blocks = 0, n_tok = 0;
   }
-  // Moves to the next unit; false at the end of the work or when the wait gave up.
+  // Moves to the next unit (whole warps only); false at the end of the work or when the wait gave up.
   template <bool kWarp>
   __device__ __forceinline__ bool next(int* err, volatile int* abort_flag) {
-    const uint32_t bar = b_full + 8 * (n % NI), parity = (n / NI) & 1;
-    if (!(kWarp ? warp_wait(bar, parity, err, abort_flag) : mbar_wait(bar, parity, err, abort_flag))) return false;
-    n_blocks = ring[n % NI].n_blocks;
-    n_tok = ring[n % NI].n_tok;
+    if (!warp_wait(b_full + 8 * (n % NI), (n / NI) & 1, err, abort_flag)) return false;
+    n_blocks = __shfl_sync(0xffffffffu, ring[n % NI].n_blocks, 0);  // the same in every lane, and known to be
+    n_tok = __shfl_sync(0xffffffffu, ring[n % NI].n_tok, 0);
     return n_blocks > 0;
   }
   __device__ __forceinline__ volatile Unit& rec() { return ring[n % NI]; }
@@ -121,7 +193,7 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               float scale_log2) {
   pdl_sync();
   extern __shared__ unsigned char smem_raw[];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int hkv = a.c.hkv, group = a.hq / hkv;
   const PagedPlanHeader* hd = static_cast<const PagedPlanHeader*>(a.plan);
   const int4 h0 = reinterpret_cast<const int4*>(hd)[0], h1 = reinterpret_cast<const int4*>(hd)[1],
@@ -142,34 +214,29 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   constexpr int kTile = tile_bytes(DH), kSub = DH / 64;
   constexpr int kSubBytes = 128 * 128;
   const uint32_t s_q = base, s_k = base + 2 * kTile, s_v = s_k + NK * kTile, s_o = s_v + NV * kTile;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(gen + (2 + NK + NV) * kTile + 16 * kStageBytes);
-  // q_full[2], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(gen + (2 + NK + NV) * kTile + 8 * kStageBytes);
+  // q_full[2], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], o_full[2], half_done[2],
+  // p_first[2], p_second[2]
   const uint32_t b_q_full = smem_u32(bars), b_q_empty = smem_u32(bars + 2);
   const uint32_t b_k_full = smem_u32(bars + 4), b_k_empty = smem_u32(bars + 6);
   const uint32_t b_v_full = smem_u32(bars + 8), b_v_empty = smem_u32(bars + 10);
-  const uint32_t b_s_full = smem_u32(bars + 12), b_p_full = smem_u32(bars + 14), b_o_full = smem_u32(bars + 16);
-  const uint32_t b_pair = smem_u32(bars + 18);                             // [8]: the two warps of a (tile, lane quarter)
-  const uint32_t b_unit_full = smem_u32(bars + 26), b_unit_empty = b_unit_full + 8 * NI;
+  const uint32_t b_s_full = smem_u32(bars + 12), b_o_full = smem_u32(bars + 14), b_half = smem_u32(bars + 16);
+  const uint32_t b_p1 = smem_u32(bars + 18), b_p2 = smem_u32(bars + 20);
+  const uint32_t b_unit_full = smem_u32(bars + 22), b_unit_empty = b_unit_full + 8 * NI;
   const uint32_t b_clc = b_unit_empty + 8 * NI, b_done = b_clc + 8;
-  const uint32_t clc_resp = smem_u32(bars + 36);                           // 16 bytes, 16-byte aligned
-  Unit* ring = reinterpret_cast<Unit*>(bars + 38);
+  const uint32_t clc_resp = smem_u32(bars + 32);                           // 16 bytes, 16-byte aligned
+  Unit* ring = reinterpret_cast<Unit*>(bars + 34);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ring + NI);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  uint32_t* votes = tmem_slot + 2;                                         // [8][3]
-  static_assert(38 * 8 + NI * sizeof(Unit) + 8 + 24 * 4 <= kBarBytes, "barrier area too small");
-  static_assert(26 + 2 * NI + 2 == 36, "barrier layout");
+  static_assert(34 * 8 + NI * sizeof(Unit) + 8 <= kBarBytes, "barrier area too small");
+  static_assert(22 + 2 * NI + 2 == 32, "barrier layout");
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 14; ++i) mbar_init(b_q_full + 8 * i, 1);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(b_p_full + 8 * i, 8);
-      mbar_init(b_o_full + 8 * i, 1);
-    }
-    for (int i = 0; i < 8; ++i) mbar_init(b_pair + 8 * i, 2);
-    for (int i = 0; i < 24; ++i) votes[i] = 0;
+    for (int i = 0; i < 18; ++i) mbar_init(b_q_full + 8 * i, 1);
+    for (int i = 0; i < 4; ++i) mbar_init(b_p1 + 8 * i, 4);  // the four warps of a tile
     for (int i = 0; i < NI; ++i) {
       mbar_init(b_unit_full + 8 * i, 1);
-      mbar_init(b_unit_empty + 8 * i, 17);  // the MMA thread and sixteen softmax warps
+      mbar_init(b_unit_empty + 8 * i, 9);  // the MMA thread and eight softmax warps
     }
     mbar_init(b_clc, 1);
     mbar_init(b_done, 1);
@@ -183,7 +250,7 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer (the whole warp)
@@ -302,117 +369,108 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
-      constexpr uint32_t kIdescS = idesc_bf16(BM, BN, 0), kIdescO = idesc_bf16(BM, DH, 1);
-      constexpr int kDepthSteps = DH / 16;
-      UnitReader its, itp;  // the block whose scores are issued next; the block whose P V is issued next
-      its.init(ring, b_unit_full, b_unit_empty);
-      itp.init(ring, b_unit_full, b_unit_empty);
-      bool s_has = its.next<false>(err, abort_flag), p_has = itp.next<false>(err, abort_flag);
-      int sj = 0, pj = 0;                               // block index inside its / itp
-      uint32_t sq[2] = {0, 0}, pc[2] = {0, 0};          // Q tiles used up; blocks whose P V has been issued, per tile
-      uint32_t kc = 0, vc = 0;
-      bool ok = true;
-      // S_x of block (its, sj).  The block's last tile also releases the keys and moves the score cursor on.
-      auto issue_s = [&](int x, int last) {
-        const uint32_t st = kc % NK;
-        if (sj == 0 && !mbar_wait(b_q_full + 8 * x, sq[x] & 1, err, abort_flag)) return false;
-        if (x == 0 && !mbar_wait(b_k_full + 8 * st, (kc / NK) & 1, err, abort_flag)) return false;
-        tc_fence_after();
-        const uint32_t aq = s_q + x * kTile, ak = s_k + st * kTile;
+    // The whole warp runs this role in step and one elected thread issues: counters, descriptors and addresses are then
+    // provably the same in all lanes, so the compiler keeps them in uniform registers, where the instructions want them.
+    constexpr uint32_t kIdescS = idesc_bf16(BM, BN, 0), kIdescO = idesc_bf16(BM, DH, 1);
+    UnitReader its, itp;  // the block whose scores are issued next; the block whose P V is issued next
+    its.init(ring, b_unit_full, b_unit_empty);
+    itp.init(ring, b_unit_full, b_unit_empty);
+    bool s_has = its.next<true>(err, abort_flag), p_has = itp.next<true>(err, abort_flag);
+    int sj = 0, pj = 0;                                 // block index inside its / itp
+    uint32_t sq0 = 0, sq1 = 0, pc0 = 0, pc1 = 0;        // Q tiles used up; blocks whose P V has been issued, per tile
+    uint32_t kc = 0, vc = 0;
+    bool ok = true;
+    // S_x of block (its, sj).  The block's last tile also releases the keys and moves the score cursor on.
+    auto issue_s = [&](int x, bool last, uint32_t& sq) {
+      const uint32_t st = kc % NK;
+      const bool end = sj == its.n_blocks - 1;
+      if (sj == 0 && !warp_wait(b_q_full + 8 * x, sq & 1, err, abort_flag)) return false;
+      if (x == 0 && !warp_wait(b_k_full + 8 * st, (kc / NK) & 1, err, abort_flag)) return false;
+      tc_fence_after();
+      const uint64_t da = smem_desc(s_q + x * kTile, 16, 1024), db = smem_desc(s_k + st * kTile, 16, 1024);
+      if (elect_one()) {
 #pragma unroll
-        for (int kk = 0; kk < kDepthSteps; ++kk) {
-          const uint64_t da = smem_desc(aq + (kk >> 2) * kSubBytes + (kk & 3) * 32, 16, 1024);
-          const uint64_t db = smem_desc(ak + (kk >> 2) * kSubBytes + (kk & 3) * 32, 16, 1024);
-          umma_bf16(tmem + x * BN, da, db, kIdescS, kk != 0);
+        for (int kk = 0; kk < DH / 16; ++kk) {
+          // a descriptor counts in 16-byte units, and shared memory ends before they overflow their field
+          const uint32_t off = ((kk >> 2) * kSubBytes + (kk & 3) * 32) >> 4;
+          umma_bf16(tmem + x * BN, da + off, db + off, kIdescS, kk != 0);
         }
         umma_commit(b_s_full + 8 * x);
-        if (sj == its.n_blocks - 1) {
-          umma_commit(b_q_empty + 8 * x);  // the unit's last use of Q_x
-          ++sq[x];
-        }
-        if (x == last) {
-          umma_commit(b_k_empty + 8 * st);
-          ++kc;
-          if (++sj == its.n_blocks) {
-            sj = 0;
-            its.advance();
-            s_has = its.next<false>(err, abort_flag);
-          }
-        }
-        return true;
-      };
-      auto issue_pv = [&](int x, int last) {
-        const uint32_t st = vc % NV;
-        if (!mbar_wait(b_p_full + 8 * x, pc[x] & 1, err, abort_flag)) return false;
-        if (x == 0 && !mbar_wait(b_v_full + 8 * st, (vc / NV) & 1, err, abort_flag)) return false;
-        tc_fence_after();
-        const uint32_t av = s_v + st * kTile;
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-          const uint64_t db = smem_desc(av + kk * 2048, kSubBytes, 1024);
-          umma_bf16_ts(tmem + 2 * BN + x * DH, tmem + x * BN + kk * 8, db, kIdescO, (pj | kk) != 0);
-        }
-        umma_commit(b_o_full + 8 * x);
-        if (x == last) umma_commit(b_v_empty + 8 * st);
-        ++pc[x];
-        return true;
-      };
-      if (s_has) {
-        const int last = its.n_tok > tpt;
-        ok = issue_s(0, last);
-        if (ok && last) ok = issue_s(1, last);
+        if (end) umma_commit(b_q_empty + 8 * x);  // the unit's last use of Q_x
+        if (last) umma_commit(b_k_empty + 8 * st);
       }
-      while (ok && p_has) {
-        const int p_last = itp.n_tok > tpt;
-        const bool s_now = s_has;
-        const int s_last = s_now && its.n_tok > tpt;
-        ok = issue_pv(0, p_last);
-        if (ok && s_now) ok = issue_s(0, s_last);
-        if (ok && p_last) ok = issue_pv(1, p_last);
-        if (ok && s_last) ok = issue_s(1, s_last);
-        ++vc;
-        if (++pj == itp.n_blocks) {
-          pj = 0;
-          itp.release();  // the score cursor is past this unit too
-          itp.advance();
-          p_has = itp.next<false>(err, abort_flag);
-        }
-      }
-      umma_commit(b_done);  // every MMA issued above has completed before the tensor memory is given back
-      mbar_drain(b_done, 0);
-    }
-  } else {
-    // ------------------------------------------------------------------ softmax + output, two threads per query row
-    const int x = (warp - 2) >> 3;         // tile A or B
-    const int hf = ((warp - 2) >> 2) & 1;  // which chunks of a block / which half of the output columns
-    const int quarter = warp & 3;          // the TMEM lane quarter this warp may access
-    const int r = quarter * 32 + lane;     // row inside the tile = TMEM lane
-    const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-    const uint32_t t_s = tmem + lane_base + x * BN, t_o = tmem + lane_base + 2 * BN + x * DH + hf * (DH / 2);
-    const uint32_t bar_s = b_s_full + 8 * x, bar_p = b_p_full + 8 * x, bar_o = b_o_full + 8 * x;
-    const int tt = r / group, head = r % group;  // token inside the tile, head of the group
-    // Meeting point of the two warps that share these 32 rows, carrying a vote: slot (u + 1) % 3 is cleared before the
-    // arrival at meeting u; both warps read it after meeting u - 2 and before arriving at u - 1.
-    const uint32_t pair_mb = b_pair + 8 * (x * 4 + quarter);
-    volatile uint32_t* my_votes = votes + 3 * (x * 4 + quarter);
-    uint32_t meet = 0;
-    auto pair_meet = [&](bool flag) -> int {
       __syncwarp();
-      const bool any = __any_sync(0xffffffffu, flag);
-      if (lane == 0) {
-        if (hf == 0) my_votes[(meet + 1) % 3] = 0;
-        if (any) my_votes[meet % 3] = 1;
-        mbar_arrive(pair_mb);
+      if (end) ++sq;
+      if (last) {
+        ++kc;
+        if (++sj == its.n_blocks) {
+          sj = 0;
+          its.advance();
+          s_has = its.next<true>(err, abort_flag);
+        }
       }
-      if (!warp_wait(pair_mb, meet & 1, err, abort_flag)) return -1;
-      const int v = (int)my_votes[meet % 3];
-      ++meet;
-      return v;
+      return true;
     };
+    // O_x += P_x V_j in two halves of 64 keys: the first runs while the second's probabilities are still being formed
+    auto issue_pv = [&](int x, bool last, uint32_t& pc) {
+      const uint32_t st = vc % NV;
+      if (!warp_wait(b_p1 + 8 * x, pc & 1, err, abort_flag)) return false;
+      if (x == 0 && !warp_wait(b_v_full + 8 * st, (vc / NV) & 1, err, abort_flag)) return false;
+      tc_fence_after();
+      const uint64_t dv = smem_desc(s_v + st * kTile, kSubBytes, 1024);
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          umma_bf16_ts(tmem + 2 * BN + x * DH, tmem + x * BN + kk * 8, dv + kk * (2048 >> 4), kIdescO, (pj | kk) != 0);
+        umma_commit(b_half + 8 * x);
+      }
+      __syncwarp();
+      if (!warp_wait(b_p2 + 8 * x, pc & 1, err, abort_flag)) return false;
+      tc_fence_after();
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 4; kk < 8; ++kk)
+          umma_bf16_ts(tmem + 2 * BN + x * DH, tmem + x * BN + kk * 8, dv + kk * (2048 >> 4), kIdescO, 1);
+        umma_commit(b_o_full + 8 * x);
+        if (last) umma_commit(b_v_empty + 8 * st);
+      }
+      __syncwarp();
+      ++pc;
+      return true;
+    };
+    if (s_has) {
+      const bool two = its.n_tok > tpt;
+      ok = issue_s(0, !two, sq0);
+      if (ok && two) ok = issue_s(1, true, sq1);
+    }
+    while (ok && p_has) {
+      const bool p_two = itp.n_tok > tpt, s_now = s_has, s_two = s_now && its.n_tok > tpt;
+      ok = issue_pv(0, !p_two, pc0);
+      if (ok && s_now) ok = issue_s(0, !s_two, sq0);
+      if (ok && p_two) ok = issue_pv(1, true, pc1);
+      if (ok && s_two) ok = issue_s(1, true, sq1);
+      ++vc;
+      if (++pj == itp.n_blocks) {
+        pj = 0;
+        if (lane == 0) itp.release();  // the score cursor is past this unit too
+        itp.advance();
+        p_has = itp.next<true>(err, abort_flag);
+      }
+    }
+    if (elect_one()) umma_commit(b_done);  // every MMA issued above has completed before the tensor memory is given back
+    mbar_drain(b_done, 0);
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------------ softmax + output, one thread per query row
+    const int x = (warp - 2) >> 2;       // tile A or B
+    const int quarter = warp & 3;        // the TMEM lane quarter this warp may access
+    const int r = quarter * 32 + lane;   // row inside the tile = TMEM lane
+    const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+    const uint32_t t_s = tmem + lane_base + x * BN, t_o = tmem + lane_base + 2 * BN + x * DH;
+    const uint32_t bar_s = b_s_full + 8 * x, bar_o = b_o_full + 8 * x;
+    const int tt = r / group, head = r % group;  // token inside the tile, head of the group
     const uint32_t stg = s_o + (uint32_t)(warp - 2) * kStageBytes;
-    const uint32_t stg_other = s_o + (uint32_t)((warp - 2) ^ 4) * kStageBytes;
-    const int c0 = hf, c1 = hf + 2;
+    const uint64_t sc2 = f2_pack(scale_log2, scale_log2);
     UnitReader it;
     it.init(ring, b_unit_full, b_unit_empty);
     uint32_t gc = 0;  // blocks of this tile handled so far
@@ -434,18 +492,18 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       const int lim_min = __reduce_min_sync(0xffffffffu, lim), lim_max = __reduce_max_sync(0xffffffffu, lim);
       const bool warp_live = __any_sync(0xffffffffu, live);
       const bool sees = lim > k0;
-      float ms = 0.f, l = 0.f;  // reference exponent; this thread's part of the row sum
+      float ms = 0.f, l = 0.f;  // reference exponent, row sum
       for (int j = 0; j < it.n_blocks; ++j, ++gc) {
         if (!warp_wait(bar_s, gc & 1, err, abort_flag)) { ok = false; break; }
         tc_fence_after();
         const int kb = k0 + j * BN;
         if (x == 0 && kb + BN > k1) {
-          // the value tile's rows behind the last key: A's eight warps clear them.  A handles every block, so block gc is
+          // the value tile's rows behind the last key: A's four warps clear them.  A handles every block, so block gc is
           // value tile gc; its scores were issued after P V(gc - 1), whose wait saw every earlier phase of v_full.
           const uint32_t st = gc % NV;
           if (!warp_wait(b_v_full + 8 * st, (gc / NV) & 1, err, abort_flag)) { ok = false; break; }
           const int first = k1 - kb, n16 = (BN - first) * (DH / 8);
-          for (int u = (warp - 2) * 32 + lane; u < n16; u += 256) {
+          for (int u = (warp - 2) * 32 + lane; u < n16; u += 128) {
             const int rr = first + u / (DH / 8), ch = u % (DH / 8);
             const uint32_t dst = s_v + st * kTile + (ch >> 3) * kSubBytes + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4);
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst), "r"(0) : "memory");
@@ -453,128 +511,113 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           fence_async_smem();
         }
         if (warp_live) {
-          uint32_t sa[32], pk[32];
-          tmem_ld32(t_s + c0 * 32, sa);
-          if (j == 0) {
-            uint32_t s00;
-            tmem_ld1(t_s, s00);
-            tmem_ld_wait();
-            ms = sees ? __uint_as_float(s00) * scale_log2 : 0.f;
-          } else {
-            tmem_ld_wait();
-          }
-          const uint64_t sc2 = f2_pack(scale_log2, scale_log2);
-          uint64_t rs2;
-          auto chunk = [&](int ch, uint32_t* cur, uint32_t* out16) {
-            const int key = kb + ch * 32;
+          // Two halves of two 32-key chunks; the next chunk's scores are on their way while this one's exponentials run.  P of
+          // half i goes over the score columns 32 i .. 32 i + 31, which have been read by then.
+          uint32_t buf[2][32], pk[32];
+          // one chunk: mask where the warp's rows need it, exponentials, sum
+          auto chunk = [&](int c, uint32_t* cur, uint32_t* out16) -> float {
+            const int key = kb + c * 32;
             if (key >= lim_max) {  // beyond every row of this warp
 #pragma unroll
-              for (int c = 0; c < 16; ++c) out16[c] = 0u;
-              return;
+              for (int e = 0; e < 16; ++e) out16[e] = 0u;
+              return 0.f;
             }
             if (key + 32 > lim_min) {
 #pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (key + c >= lim) cur[c] = 0xff800000u;  // -inf
+              for (int e = 0; e < 32; ++e)
+                if (key + e >= lim) cur[e] = 0xff800000u;  // -inf
             }
-            const uint64_t nm2 = f2_pack(-ms, -ms);
-#pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              float x0, x1;
-              f2_unpack(f2_fma(f2_pack(__uint_as_float(cur[2 * c]), __uint_as_float(cur[2 * c + 1])), sc2, nm2), x0, x1);
-              const float p0 = ex2(x0), p1 = ex2(x1);
-              rs2 = f2_add(rs2, f2_pack(p0, p1));
-              out16[c] = pack_bf16(p0, p1);
-            }
+            float sum;
+            exp_chunk(cur, sc2, ms, out16, sum);
+            return sum;
           };
-          rs2 = f2_pack(0.f, 0.f);
-          chunk(c0, sa, pk);
-          tmem_ld32(t_s + c1 * 32, sa);
-          tmem_ld_wait();
-          chunk(c1, sa, pk + 16);
-          float rlo, rhi;
-          f2_unpack(rs2, rlo, rhi);
-          float rs = rlo + rhi;
-          // The vote "some row sum is out of range" also orders the P stores below after both threads' score loads.
-          const int vote = pair_meet(live && !(rs <= kBigSum));
-          if (vote < 0) { ok = false; break; }
-          if (vote) {
-            // Rare: rows whose largest exponent is beyond 2^64 move their reference up by d = ceil(that exponent); what
-            // was accumulated is scaled by 2^-d (exact).  Nothing of this block has been stored yet.
-            float xmax = -INFINITY;
-#pragma unroll 1
-            for (int v = 0; v < 2; ++v) {
-              const int ch = v ? c1 : c0;
-              tmem_ld32(t_s + ch * 32, sa);
-              tmem_ld_wait();
+          tmem_ld32(t_s, buf[0]);
+          tmem_ld_wait32(buf[0]);
+          if (j == 0) ms = sees ? __uint_as_float(buf[0][0]) * scale_log2 : 0.f;
 #pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (kb + ch * 32 + c < lim) xmax = fmaxf(xmax, fmaf(__uint_as_float(sa[c]), scale_log2, -ms));
-            }
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(stg + lane * 4), "f"(xmax) : "memory");
-            if (pair_meet(false) < 0) { ok = false; break; }
-            float xo;
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(xo) : "r"(stg_other + lane * 4) : "memory");
-            xmax = fmaxf(xmax, xo);
-            const float d = xmax > 64.f ? ceilf(xmax) : 0.f;
-            const float f = exp2f(-d);
-            if (j > 0) {
-              if (!warp_wait(bar_o, (gc - 1) & 1, err, abort_flag)) { ok = false; break; }  // complete already
-              tc_fence_after();
+          for (int i = 0; i < 2; ++i) {
+            if (i == 1) tmem_ld_wait32(buf[0]);
+            tmem_ld32(t_s + (2 * i + 1) * 32, buf[1]);
+            float sum = chunk(2 * i, buf[0], pk);
+            tmem_ld_wait32(buf[1]);
+            if (i == 0) tmem_ld32(t_s + 64, buf[0]);
+            sum += chunk(2 * i + 1, buf[1], pk + 16);
+            if (__any_sync(0xffffffffu, live && !(sum <= kBigSum))) {
+              // Rare: rows whose largest exponent is beyond 2^64 move their reference up by d = ceil(that exponent); what was
+              // accumulated under the old one is scaled by 2^-d (exact).  This half's P has not been stored, so its scores
+              // are still there; the other half's product, if it was issued, has to be in O first.
+              if (i == 0) tmem_ld_wait32(buf[0]);
+              float xmax = -INFINITY;
 #pragma unroll 1
-              for (int c = 0; c < DH / 64; ++c) {
-                uint32_t o[32];
-                tmem_ld32(t_o + c * 32, o);
+              for (int v = 0; v < 4; ++v) {
+                uint32_t o[16];
+                tmem_ld16(t_s + i * 64 + v * 16, o);
                 tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                tmem_st32(t_o + c * 32, o);
+                for (int e = 0; e < 16; ++e)
+                  if (kb + i * 64 + v * 16 + e < lim) xmax = fmaxf(xmax, fmaf(__uint_as_float(o[e]), scale_log2, -ms));
               }
+              const float d = xmax > 64.f ? ceilf(xmax) : 0.f;
+              const float f = exp2f(-d);
+              if (i == 1) {
+                if (!warp_wait(b_half + 8 * x, gc & 1, err, abort_flag)) { ok = false; break; }
+                tc_fence_after();
+              }
+              if (j > 0 || i == 1) {
+#pragma unroll 1
+                for (int v = 0; v < DH / 16; ++v) {
+                  uint32_t o[16];
+                  tmem_ld16(t_o + v * 16, o);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                  tmem_st16(t_o + v * 16, o);
+                }
+                tmem_st_wait();
+              }
+              l *= f;
+              ms += d;
+              tmem_ld32(t_s + 2 * i * 32, buf[0]);
+              tmem_ld_wait32(buf[0]);
+              sum = chunk(2 * i, buf[0], pk);
+              tmem_ld32(t_s + (2 * i + 1) * 32, buf[1]);
+              tmem_ld_wait32(buf[1]);
+              sum += chunk(2 * i + 1, buf[1], pk + 16);
+              if (i == 0) tmem_ld32(t_s + 64, buf[0]);
             }
-            l *= f;
-            ms += d;
-            rs2 = f2_pack(0.f, 0.f);
-            tmem_ld32(t_s + c0 * 32, sa);
-            tmem_ld_wait();
-            chunk(c0, sa, pk);
-            tmem_ld32(t_s + c1 * 32, sa);
-            tmem_ld_wait();
-            chunk(c1, sa, pk + 16);
-            f2_unpack(rs2, rlo, rhi);
-            rs = rlo + rhi;
-            if (pair_meet(false) < 0) { ok = false; break; }  // the partner has re-read its scores too
+            l += sum;
+            tmem_st32(t_s + i * 32, pk);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive((i == 0 ? b_p1 : b_p2) + 8 * x);
           }
-          l += rs;
-          tmem_st16(t_s + c0 * 16, pk);
-          tmem_st16(t_s + c1 * 16, pk + 16);
-          tmem_st_wait();
+          if (!ok) break;
+        } else {
+          // no live row: the barriers' phases only (whatever P holds reaches rows that nobody stores)
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(b_p1 + 8 * x);
+            mbar_arrive(b_p2 + 8 * x);
+          }
         }
-        tc_fence_before();
-        // The scores of block gc were issued after the wait for p_full(gc - 1), so that phase is over before any warp
-        // gets here.
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_p);
       }
       if (!ok) break;
       if (!warp_wait(bar_o, (gc - 1) & 1, err, abort_flag)) { ok = false; break; }
       tc_fence_after();
       if (warp_live) {
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(stg + lane * 4), "f"(l) : "memory");
-        if (pair_meet(false) < 0) { ok = false; break; }
-        float lo;
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(lo) : "r"(stg_other + lane * 4) : "memory");
-        if (pair_meet(false) < 0) { ok = false; break; }  // read before either warp stages output there
         if (part < 0) {
-          // This thread's columns of O_x / l as bf16, 32 at a time through the warp's staging rows (64 bytes each,
-          // 16-byte pieces XOR-swizzled), so that global stores are 64 contiguous bytes per row.
-          const float inv = 1.f / (l + lo);
+          // This row's O_x / l as bf16, 32 columns at a time through the warp's staging rows (64 bytes each, 16-byte
+          // pieces XOR-swizzled), so that global stores are 64 contiguous bytes per row.
+          const float inv = 1.f / l;
           const long long at = live ? (long long)(row0 + x * tpt + tt) * a.out_stride + (long long)(h * group + head) * DH : -1;
-          __nv_bfloat16* ocol = static_cast<__nv_bfloat16*>(a.out) + hf * (DH / 2);
+          __nv_bfloat16* ocol = static_cast<__nv_bfloat16*>(a.out);
 #pragma unroll 1
-          for (int pt = 0; pt < DH / 64; ++pt) {
+          for (int pt = 0; pt < DH / 32; ++pt) {
             uint32_t o[32];
             tmem_ld32(t_o + pt * 32, o);
-            tmem_ld_wait();
+            tmem_ld_wait32(o);
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               const uint32_t dst = stg + lane * 64 + ((v ^ ((lane >> 1) & 3)) << 4);
@@ -605,18 +648,18 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           float* p = a.ws + ((long long)part * hkv + h) * paged_part_floats(256, DH);
           const int rc = x * tpt * group + r;  // (token, head) index inside the unit
 #pragma unroll 1
-          for (int pt = 0; pt < DH / 64; ++pt) {
+          for (int pt = 0; pt < DH / 32; ++pt) {
             uint32_t o[32];
             tmem_ld32(t_o + pt * 32, o);
-            tmem_ld_wait();
+            tmem_ld_wait32(o);
             if (live) {
 #pragma unroll
               for (int v = 0; v < 8; ++v)
-                *reinterpret_cast<uint4*>(p + ((long long)(hf * (DH / 8) + pt * 8 + v) * 256 + rc) * 4) =
+                *reinterpret_cast<uint4*>(p + ((long long)(pt * 8 + v) * 256 + rc) * 4) =
                     make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
             }
           }
-          if (live && hf == 0) *reinterpret_cast<float2*>(p + 256 * DH + 2 * rc) = make_float2(ms, l + lo);
+          if (live) *reinterpret_cast<float2*>(p + 256 * DH + 2 * rc) = make_float2(ms, l);
         }
       }
       // The next unit's first P V (which overwrites O_x) is issued only after this thread's arrival for that block.

@@ -56,6 +56,10 @@ template <int DH>
 __global__ void __launch_bounds__(kThreads, 2)
 k_paged_tokens(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                const __grid_constant__ PagedAttnArgs a, int shift, float scale_log2) {
+  if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+  }
   pdl_sync();
   constexpr int kStages = n_stages(DH), kStage = stage_bytes(DH), kHalf = kStage / 2;
   constexpr int NK = DH / 16, NO = DH / 8;  // MMA steps over head_dim; 8-column tiles of the output
@@ -65,6 +69,8 @@ k_paged_tokens(const __grid_constant__ CUtensorMap map_k, const __grid_constant_
   const int item = blockIdx.x / hkv, h = blockIdx.x % hkv;
   const int4 h0 = reinterpret_cast<const int4*>(hd)[0], h1 = reinterpret_cast<const int4*>(hd)[1],
              h2 = reinterpret_cast<const int4*>(hd)[2];
+  // the grid is not larger than the list's room, so the item can be fetched beside the header that says whether it exists
+  PagedItem it = paged_item_raw(hd, item);
   if (h0.x != kPagedTokens || h1.x != a.hq || h1.y != hkv || h1.z != DH || h1.w != a.total_q || h2.x != a.n_seq ||
       h2.y != a.max_q) {
     if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(a.err, kErrBadOffsets);
@@ -73,7 +79,7 @@ k_paged_tokens(const __grid_constant__ CUtensorMap map_k, const __grid_constant_
   // more items than the launch was sized for: lengths beyond the block table's width
   if (threadIdx.x == 0 && blockIdx.x == 0 && h0.y * hkv > (int)gridDim.x) atomicOr(a.err, kErrBadPage);
   if (item >= h0.y) return;
-  const PagedItem it = paged_item(hd, item, a.max_pages, shift, a.ws, a.err);
+  paged_item_check(it, a.max_pages, shift, a.ws, a.err);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   unsigned char* gen = smem_raw + (base - raw);

@@ -12,6 +12,7 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
+constexpr int kRowsHere = 16384;
 
 __device__ __forceinline__ unsigned cluster_rank() {
   unsigned r;
@@ -72,13 +73,15 @@ __device__ __forceinline__ int find_row(const int* start, int n, int x) {
 
 // Pages and slots for the new tokens of every sequence.  One cluster: every block scans the lengths for itself (at most
 // 4096 of them), the blocks meet once, so that lengths and pool size may be updated in place, and then share the writes.
-// Bound by latency (two dependent loads, two scans of 1024 threads, the meeting) up to some ten thousand rows and by the
-// stores of the few SMs behind that; a cluster instead of a grid keeps it at one launch without any counter that outlives it.
+// Bound by latency (two dependent loads, two scans of 1024 threads, the meeting); a cluster instead of a grid keeps it at one
+// launch without any counter that outlives it.  Many rows would be bound by the searches and stores of eight SMs: above
+// kRowsHere rows they are left to k_page_rows.
 __global__ void __launch_bounds__(kThreads) k_page_append(const int* len_new, const int* kv_in, int* kv_out, int n, int shift,
                                                           int num_pages, int max_pages, long long table_stride,
                                                           int* table, const int* __restrict__ free_pages,
                                                           const int* n_free_in, int* n_free_out, int total, int* cu, int* pos,
-                                                          int* slot, int* err, int vec) {
+                                                          int* slot, int* err, int vec, int rows_here) {
+  pdl_sync();
   extern __shared__ int sm[];
   int* s_cu = sm;               // [n + 1] first row of each sequence
   int* s_first = s_cu + n + 1;  // [n + 1] first new page of each sequence, counted over the call
@@ -132,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) k_page_append(const int* len_new, co
     table[s * table_stride + j] = id;
   }
   // rows, four at a time: one search serves them, and they leave as 16-byte stores
-  const int quads = (int)(((long long)total + 3) >> 2);
+  const int quads = rows_here ? (int)(((long long)total + 3) >> 2) : 0;
   for (int u = gid; u < quads; u += step) {
     const int t0 = u * 4, t1 = min(total, t0 + 4);
     int s = t0 < rows ? find_row(s_cu, n, t0) : n - 1;
@@ -160,6 +163,45 @@ __global__ void __launch_bounds__(kThreads) k_page_append(const int* len_new, co
     } else {
       for (int e = 0; e < t1 - t0; ++e) pos[t0 + e] = ps[e], slot[t0 + e] = sl[e];
     }
+  }
+  if (bad_page) atomicOr(err, kErrBadPage);
+}
+
+// The rows of a large append, over the whole GPU: everything they need is in the first kernel's outputs (cu, kv_out and the
+// table with its new entries; a refused call left cu = 0, which makes every row padding).
+__global__ void __launch_bounds__(256) k_page_rows(const int* __restrict__ cu, const int* __restrict__ kv_out, int n, int shift,
+                                                   int num_pages, long long table_stride, const int* __restrict__ table,
+                                                   int total, int* __restrict__ pos, int* __restrict__ slot, int* err, int vec) {
+  pdl_sync();
+  const int page = 1 << shift, rows = cu[n];
+  const int t0 = (int)min((long long)total, 4ll * ((long long)blockIdx.x * 256 + threadIdx.x)), t1 = min(total, t0 + 4);
+  if (t0 >= total) return;
+  int s = t0 < rows ? find_row(cu, n, t0) : n - 1;
+  int ps[4], sl[4], beg = 0, end = 0, kv = 0, last = -1, id = -1;
+  bool bad_page = false;
+  if (t0 < rows) beg = cu[s], end = cu[s + 1], kv = kv_out[s] - (end - beg);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int t = t0 + e;
+    ps[e] = 0, sl[e] = -1;
+    if (t < rows) {
+      while (t >= end) {
+        ++s, last = -1;
+        beg = end, end = cu[s + 1], kv = kv_out[s] - (end - beg);
+      }
+      const int p = kv + t - beg, j = p >> shift;
+      if (j != last) id = table[s * table_stride + j], last = j;
+      ps[e] = p;
+      const bool out = (unsigned)id >= (unsigned)num_pages;
+      bad_page |= out;
+      sl[e] = out ? -1 : (id << shift) + (p & (page - 1));
+    }
+  }
+  if (vec && t0 + 4 <= total) {
+    *reinterpret_cast<int4*>(pos + t0) = make_int4(ps[0], ps[1], ps[2], ps[3]);
+    *reinterpret_cast<int4*>(slot + t0) = make_int4(sl[0], sl[1], sl[2], sl[3]);
+  } else {
+    for (int e = 0; e < t1 - t0; ++e) pos[t0 + e] = ps[e], slot[t0 + e] = sl[e];
   }
   if (bad_page) atomicOr(err, kErrBadPage);
 }
@@ -302,26 +344,28 @@ __global__ void __launch_bounds__(128) k_qknorm_rope_paged(const T* qkv, long lo
   constexpr int V = Vec16<T>::N;
   __shared__ __align__(16) float s_cos[128], s_sin[128];
   const int row = blockIdx.x, dh = c.dh, half = dh >> 1, heads = hq + 2 * c.hkv;
-  const int slot = slot_map[row];
+  const int slot = slot_map[row], p = pos[row];
+  const int per_block = 128 / lanes;  // heads a pass of the block covers
+  const int sub = threadIdx.x & (lanes - 1), h_first = threadIdx.x / lanes;
+  const bool live = sub * V < half;  // lanes of a head are rounded up to a power of two
+  const T* src = qkv + row * qkv_stride;
+  // two passes ahead: at 16 + 8 + 8 heads of 128 the whole row is in flight before anything waits
+  uint4 ua[2], ub[2];
+  auto fetch = [&](int h, int i) {
+    ua[i] = ub[i] = make_uint4(0, 0, 0, 0);
+    if (h < heads && live) {
+      ua[i] = *reinterpret_cast<const uint4*>(src + (long long)h * dh + sub * V);
+      ub[i] = *reinterpret_cast<const uint4*>(src + (long long)h * dh + half + sub * V);
+    }
+  };
+  fetch(h_first, 0);
+  fetch(h_first + per_block, 1);
   if (slot < 0) return;  // a padding row: nothing is written for it
   const int page = slot >> shift, off = slot & ((1 << shift) - 1);
   if (page >= c.num_pages) {
     if (threadIdx.x == 0) atomicOr(err, kErrBadPage);
     return;
   }
-  const int per_block = 128 / lanes;  // heads a pass of the block covers
-  const int sub = threadIdx.x & (lanes - 1), h_first = threadIdx.x / lanes;
-  const bool live = sub * V < half;  // lanes of a head are rounded up to a power of two
-  const T* src = qkv + row * qkv_stride;
-  uint4 ua = make_uint4(0, 0, 0, 0), ub = ua;
-  auto fetch = [&](int h) {
-    if (h < heads && live) {
-      ua = *reinterpret_cast<const uint4*>(src + (long long)h * dh + sub * V);
-      ub = *reinterpret_cast<const uint4*>(src + (long long)h * dh + half + sub * V);
-    }
-  };
-  fetch(h_first);
-  const int p = pos[row];
   for (int j = threadIdx.x; j < half; j += 128) {
     double t = p * freq.turns[j];
     t -= rint(t);                              // [-1/2, 1/2] turns
@@ -340,8 +384,9 @@ __global__ void __launch_bounds__(128) k_qknorm_rope_paged(const T* qkv, long lo
   // every lane of a warp takes the same number of passes, so the shuffles below always have all of them
   for (int h0 = 0; h0 < heads; h0 += per_block) {
     const int h = h0 + h_first;
-    uint4 xa = ua, xb = ub;
-    fetch(h + per_block);
+    uint4 xa = ua[0], xb = ub[0];
+    ua[0] = ua[1], ub[0] = ub[1];
+    fetch(h + 2 * per_block, 1);
     float a[V], b[V];
     unpack16<T>(xa, a);
     unpack16<T>(xb, b);
@@ -420,9 +465,23 @@ cudaError_t launch_page_append(const int* len_new, const int* kv_in, int* kv_out
   static std::atomic<unsigned long long> set;
   if (cudaError_t e = ensure_dynamic_smem(k_page_append, (3 * kMaxCandidates + 2) * (int)sizeof(int), set)) return e;
   const int vec = !((reinterpret_cast<uintptr_t>(pos) | reinterpret_cast<uintptr_t>(slot)) & 15);
-  return launch_cluster(k_page_append, cluster_blocks(total, 4 * kThreads), smem, st, len_new, kv_in, kv_out, n,
-                        log2_of(page_size), num_pages, max_pages, table_stride, table, free_pages, n_free_in, n_free_out, total,
-                        cu, pos, slot, err, vec);
+  const int shift = log2_of(page_size);
+  const int rows_here = total <= kRowsHere;
+  cudaError_t e = launch_cluster(k_page_append, cluster_blocks(rows_here ? total : total / 8, 4 * kThreads), smem, st, len_new,
+                                 kv_in, kv_out, n, shift, num_pages, max_pages, table_stride, table, free_pages, n_free_in,
+                                 n_free_out, total, cu, pos, slot, err, vec, rows_here);
+  if (e != cudaSuccess || rows_here) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(((long long)total + 1023) / 1024));
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_enabled() ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, k_page_rows, (const int*)cu, (const int*)kv_out, n, shift, num_pages, table_stride,
+                            (const int*)table, total, pos, slot, err, vec);
 }
 
 cudaError_t launch_page_release(const int* keep, int n_new, const int* kv_in, int* kv_out, int n, int page_size, int num_pages,

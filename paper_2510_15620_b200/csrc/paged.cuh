@@ -32,7 +32,11 @@ struct PagedPlanShape {
   int tokens;      // tokens an item covers
   int min_piece;   // keys: tiles are never cut into pieces shorter than this
   int piece_unit;  // keys: pieces are multiples of this
-  int target;      // pieces (times key/value heads) the whole launch is cut into when it is short of items
+  int target;      // pieces are at least total keys * hkv / target long
+  int slots;       // blocks that run at a time
+  // What a launch is expected to take, in nanoseconds (measured): per key of a block's own, at least, and per key and running
+  // block (they share the memory's rate); per item; per piece of a cut tile; once if any tile is cut.
+  float ns_key, ns_key_block, ns_item, ns_part, ns_join;
 };
 
 // Work list of one step: header, items, joins.  A tile of query rows whose keys are cut into pieces has one item per
@@ -48,20 +52,26 @@ struct PagedItem {
   int k0, k1, part, pad;       // keys [k0, k1) of the sequence; partial result or -1
 };
 #ifdef __CUDACC__
-// Item i, its keys cut to what the block table can name (a list made from lengths beyond it must not keep a kernel busy).
+// Cuts an item's keys to what the block table can name (a list made from lengths beyond it must not keep a kernel busy).
 // Without a workspace (a table too narrow for any tile to be cut) a cut tile can only come from such lengths too: its rows
 // become zero.  Called by whole blocks or by one warp of a block whose first thread belongs to it.
-__device__ __forceinline__ PagedItem paged_item(const PagedPlanHeader* hd, int i, int max_pages, int shift, const float* ws,
-                                                int* err) {
-  const int4* p = reinterpret_cast<const int4*>(reinterpret_cast<const PagedItem*>(hd + 1) + i);
-  const int4 a = p[0], b = p[1];
-  PagedItem it{a.x, a.y, a.z, a.w, b.x, b.y, b.z, 0};
+__device__ __forceinline__ void paged_item_check(PagedItem& it, int max_pages, int shift, const float* ws, int* err) {
   const long long cap = (long long)max_pages << shift;
   if (it.k1 > cap) {
     if (threadIdx.x == 0) atomicOr(err, kErrBadPage);
     it.k1 = (int)cap;
   }
   if (it.part >= 0 && !ws) it.k1 = it.k0 = 0, it.part = -1;
+}
+__device__ __forceinline__ PagedItem paged_item_raw(const PagedPlanHeader* hd, int i) {
+  const int4* p = reinterpret_cast<const int4*>(reinterpret_cast<const PagedItem*>(hd + 1) + i);
+  const int4 a = p[0], b = p[1];
+  return PagedItem{a.x, a.y, a.z, a.w, b.x, b.y, b.z, 0};
+}
+__device__ __forceinline__ PagedItem paged_item(const PagedPlanHeader* hd, int i, int max_pages, int shift, const float* ws,
+                                                int* err) {
+  PagedItem it = paged_item_raw(hd, i);
+  paged_item_check(it, max_pages, shift, ws, err);
   return it;
 }
 #endif

@@ -6,7 +6,7 @@ import ctypes as C
 
 import torch
 
-from .binding import PRISM_BF16, PRISM_IMPL_AUTO, PrismError, lib, _ProbeRecord
+from .binding import PRISM_BF16, PRISM_FP32, PRISM_IMPL_AUTO, PrismError, lib, _ProbeRecord
 
 _proto_done = False
 
@@ -159,86 +159,116 @@ def prism_op_compact(x_old, x_new, cu_old, cu_new, old_of_new, n_new, total_new)
 # ---- paged key/value cache.  Block tables are int32 [n_seq, max_pages] (rows may be strided), caches
 # [num_pages, n_kv_heads, page_size, head_dim] (pages may be strided, what lies inside a page may not), matrices [rows, width]
 # (rows may be strided).  A tensor of another element type or layout, or on another device than the current one, is refused:
-# the kernels would read past it.
-def _refuse_unless(ok, what):
-    if not ok:
-        raise PrismError(-1, what)
+# the kernels would read past it.  These checks are on the path of calls that run for a few microseconds, so they are plain
+# comparisons without intermediate objects.
+_I32 = torch.int32
+_ELEMENT = {PRISM_BF16: torch.bfloat16, PRISM_FP32: torch.float32}
 
 
-def _here(what, *tensors):
-    devices = {t.get_device() for t in tensors if t is not None}  # -1: host memory
-    _refuse_unless(len(devices) == 1 and -1 not in devices and torch.cuda.current_device() in devices,
-                   what + ": a tensor is not on the current device")
+def _device(what, t):
+    """Index of the current device, which t has to be on; every other tensor is compared with it."""
+    dev = t.get_device()  # -1: host memory
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise PrismError(-1, what + ": a tensor is not on the current device")
+    return dev
 
 
-def _ints(what, *pairs):
+def _stream_of(dev):
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _ints(what, dev, *pairs):
     for t, n in pairs:
-        _refuse_unless(t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= n, what + ": int32, contiguous, long enough")
+        if t.dtype is not _I32 or t.get_device() != dev or not t.is_contiguous() or t.numel() < n:
+            raise PrismError(-1, what + ": int32 tensors on the current device, contiguous and long enough")
 
 
-def _rows(what, t, dtype, width=None):
-    _refuse_unless(t.dim() == 2 and t.dtype == (torch.bfloat16 if dtype == PRISM_BF16 else torch.float32) and
-                   (t.shape[1] == width or width is None) and (t.stride(1) == 1 or t.numel() <= 1),
-                   what + ": matrix of the stated element type and width, rows without gaps inside")
+def _row_stride(t):
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
 
 
-def _table(what, t, n):
-    _refuse_unless(t.dim() == 2 and t.dtype == torch.int32 and t.shape[0] >= n and (t.stride(1) == 1 or t.shape[1] <= 1 or t.numel() == 0),
-                   what + ": int32 block table with a row per sequence")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+def _matrix(what, dev, t, dtype, width, rows=0):
+    if (t.dim() != 2 or t.dtype is not _ELEMENT.get(dtype) or t.get_device() != dev or t.shape[1] != width or t.shape[0] < rows or
+            (t.stride(1) != 1 and t.numel() > 1)):
+        raise PrismError(-1, what + ": a matrix of the stated element type, width and rows, without gaps inside a row")
+    return _row_stride(t)
 
 
-def _cache(what, k, v, dtype):
-    _refuse_unless(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype ==
-                   (torch.bfloat16 if dtype == PRISM_BF16 else torch.float32), what + ": k and v caches of one layout")
+def _table(what, dev, t, n):
+    if (t.dim() != 2 or t.dtype is not _I32 or t.get_device() != dev or t.shape[0] < n or
+            (t.stride(1) != 1 and t.shape[1] > 1 and t.numel() > 0)):
+        raise PrismError(-1, what + ": an int32 block table with a row per sequence")
+    return _row_stride(t)
+
+
+def _bytes(what, dev, t):
+    if t.get_device() != dev or not t.is_contiguous():
+        raise PrismError(-1, what + ": plan and workspace contiguous on the current device")
+    return t.numel() * t.element_size()
+
+
+def _cache(what, dev, k, v, dtype):
+    if (k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype is not _ELEMENT.get(dtype) or
+            v.dtype is not k.dtype or k.get_device() != dev or v.get_device() != dev):
+        raise PrismError(-1, what + ": k and v caches of one layout and the stated element type")
     pages, heads, page, dh = k.shape
-    _refuse_unless(k[:1].is_contiguous(), what + ": a page of the cache has gaps inside")
-    stride = k.stride(0) if pages > 1 else heads * page * dh
-    return _KvCache(_p(k), _p(v), stride, pages, page, heads, dh, dtype)
+    s0, s1, s2, s3 = k.stride()
+    if s3 != 1 or s2 != dh or (s1 != page * dh and heads > 1):
+        raise PrismError(-1, what + ": a page of the cache has gaps inside")
+    return _KvCache(k.data_ptr(), v.data_ptr(), s0 if pages > 1 else heads * page * dh, pages, page, heads, dh, dtype)
 
 
 def prism_op_page_append(len_new, kv_len_in, kv_len_out, page_size, num_pages, block_table, free_pages, n_free_in, n_free_out,
                          cu_q, pos, slot_map, err_word):
-    n, total = len_new.numel(), slot_map.numel()
-    _here("page_append", len_new, kv_len_in, kv_len_out, block_table, free_pages, n_free_in, n_free_out, cu_q, pos, slot_map,
-          err_word)
-    _ints("page_append", (len_new, n), (kv_len_in, n), (kv_len_out, n), (free_pages, num_pages), (n_free_in, 1), (n_free_out, 1),
+    what = "page_append"
+    n, total, dev = len_new.numel(), slot_map.numel(), _device(what, err_word)
+    _ints(what, dev, (len_new, n), (kv_len_in, n), (kv_len_out, n), (free_pages, num_pages), (n_free_in, 1), (n_free_out, 1),
           (cu_q, n + 1), (pos, total), (slot_map, total), (err_word, 1))
-    stride = _table("page_append", block_table, n)
-    _check(_L().prism_op_page_append(_p(len_new), _p(kv_len_in), _p(kv_len_out), n, page_size, num_pages, block_table.shape[1],
-                                     stride, _p(block_table), _p(free_pages), _p(n_free_in), _p(n_free_out), total, _p(cu_q),
-                                     _p(pos), _p(slot_map), _p(err_word), _stream()), "page_append")
+    stride = _table(what, dev, block_table, n)
+    rc = _L().prism_op_page_append(len_new.data_ptr(), kv_len_in.data_ptr(), kv_len_out.data_ptr(), n, page_size, num_pages,
+                                   block_table.shape[1], stride, block_table.data_ptr(), free_pages.data_ptr(),
+                                   n_free_in.data_ptr(), n_free_out.data_ptr(), total, cu_q.data_ptr(), pos.data_ptr(),
+                                   slot_map.data_ptr(), err_word.data_ptr(), _stream_of(dev))
+    if rc:
+        raise PrismError(rc, what)
 
 
 def prism_op_page_release(old_of_new, kv_len_in, kv_len_out, page_size, num_pages, shared_pages, table_in, table_out, free_pages,
                           n_free_in, n_free_out, err_word, n_new=None):
     """n_new: survivors (default: all of old_of_new, which may be a longer buffer)."""
-    n, n_new = kv_len_in.numel(), old_of_new.numel() if n_new is None else n_new
-    _here("page_release", old_of_new, kv_len_in, kv_len_out, table_in, table_out, free_pages, n_free_in, n_free_out, err_word)
-    _ints("page_release", (old_of_new, n_new), (kv_len_in, n), (kv_len_out, n), (free_pages, num_pages), (n_free_in, 1),
-          (n_free_out, 1), (err_word, 1))
-    s_in, s_out = _table("page_release", table_in, n), _table("page_release", table_out, n)
-    _refuse_unless(table_out.shape[1] == table_in.shape[1], "page_release: tables of one width")
-    _check(_L().prism_op_page_release(_p(old_of_new), n_new, _p(kv_len_in), _p(kv_len_out), n, page_size, num_pages, shared_pages,
-                                      table_in.shape[1], s_in, _p(table_in), s_out, _p(table_out), _p(free_pages),
-                                      _p(n_free_in), _p(n_free_out), _p(err_word), _stream()), "page_release")
+    what = "page_release"
+    n, n_new, dev = kv_len_in.numel(), old_of_new.numel() if n_new is None else n_new, _device(what, err_word)
+    _ints(what, dev, (old_of_new, n_new), (kv_len_in, n), (kv_len_out, n), (free_pages, num_pages), (n_free_in, 1), (n_free_out, 1),
+          (err_word, 1))
+    s_in, s_out = _table(what, dev, table_in, n), _table(what, dev, table_out, n)
+    if table_out.shape[1] != table_in.shape[1]:
+        raise PrismError(-1, what + ": tables of one width")
+    rc = _L().prism_op_page_release(old_of_new.data_ptr(), n_new, kv_len_in.data_ptr(), kv_len_out.data_ptr(), n, page_size,
+                                    num_pages, shared_pages, table_in.shape[1], s_in, table_in.data_ptr(), s_out,
+                                    table_out.data_ptr(), free_pages.data_ptr(), n_free_in.data_ptr(), n_free_out.data_ptr(),
+                                    err_word.data_ptr(), _stream_of(dev))
+    if rc:
+        raise PrismError(rc, what)
 
 
 def prism_op_qknorm_rope_paged(qkv, dtype, pos, slot_map, n_q_heads, qk_norm, g_q, g_k, eps, theta, q_out, k_cache, v_cache,
                                err_word):
     what = "qknorm_rope_paged"
-    _here(what, qkv, pos, slot_map, g_q, g_k, q_out, k_cache, v_cache, err_word)
-    c = _cache(what, k_cache, v_cache, dtype)
+    dev = _device(what, err_word)
+    c = _cache(what, dev, k_cache, v_cache, dtype)
     rows = qkv.shape[0]
-    s_in = _rows(what, qkv, dtype, (n_q_heads + 2 * c.n_kv_heads) * c.head_dim)
-    s_out = _rows(what, q_out, dtype, n_q_heads * c.head_dim)
-    _refuse_unless(q_out.shape[0] >= rows, what + ": a row of q_out for every row of qkv")
-    _ints(what, (pos, rows), (slot_map, rows), (err_word, 1))
-    for g in (g_q, g_k) if qk_norm else ():
-        _refuse_unless(g is not None and g.dtype == qkv.dtype and g.is_contiguous() and g.numel() == c.head_dim, what + ": gains")
-    _check(_L().prism_op_qknorm_rope_paged(_p(qkv), s_in, _p(pos), _p(slot_map), rows, n_q_heads, qk_norm, _p(g_q), _p(g_k), eps,
-                                           theta, _p(q_out), s_out, C.byref(c), _p(err_word), _stream()), what)
+    s_in = _matrix(what, dev, qkv, dtype, (n_q_heads + 2 * c.n_kv_heads) * c.head_dim)
+    s_out = _matrix(what, dev, q_out, dtype, n_q_heads * c.head_dim, rows)
+    _ints(what, dev, (pos, rows), (slot_map, rows), (err_word, 1))
+    if qk_norm:
+        for g in (g_q, g_k):
+            if g.dtype is not qkv.dtype or g.get_device() != dev or not g.is_contiguous() or g.numel() != c.head_dim:
+                raise PrismError(-1, what + ": gains of head_dim elements of the stated type")
+    rc = _L().prism_op_qknorm_rope_paged(qkv.data_ptr(), s_in, pos.data_ptr(), slot_map.data_ptr(), rows, n_q_heads, qk_norm,
+                                         _p(g_q), _p(g_k), eps, theta, q_out.data_ptr(), s_out, c, err_word.data_ptr(),
+                                         _stream_of(dev))
+    if rc:
+        raise PrismError(rc, what)
 
 
 def prism_op_attention_paged_bytes(n_seq, total_q, max_q_len, n_q_heads, n_kv_heads, head_dim, dtype, impl=PRISM_IMPL_AUTO):
@@ -251,30 +281,31 @@ def prism_op_attention_paged_bytes(n_seq, total_q, max_q_len, n_q_heads, n_kv_he
 
 def prism_op_attention_paged_plan(cu_q, kv_len, total_q, max_q_len, n_q_heads, n_kv_heads, head_dim, dtype, causal, plan, err_word,
                                   impl=PRISM_IMPL_AUTO):
-    n = kv_len.numel()
-    _here("attention_paged_plan", cu_q, kv_len, plan, err_word)
-    _ints("attention_paged_plan", (cu_q, n + 1), (kv_len, n), (err_word, 1))
-    _refuse_unless(plan.is_contiguous(), "attention_paged_plan: plan")
-    _check(_L().prism_op_attention_paged_plan(_p(cu_q), _p(kv_len), n, total_q, max_q_len, n_q_heads, n_kv_heads, head_dim, dtype,
-                                              causal, impl, _p(plan), plan.numel() * plan.element_size(), _p(err_word),
-                                              _stream()), "attention_paged_plan")
+    what = "attention_paged_plan"
+    n, dev = kv_len.numel(), _device(what, err_word)
+    _ints(what, dev, (cu_q, n + 1), (kv_len, n), (err_word, 1))
+    rc = _L().prism_op_attention_paged_plan(cu_q.data_ptr(), kv_len.data_ptr(), n, total_q, max_q_len, n_q_heads, n_kv_heads,
+                                            head_dim, dtype, causal, impl, plan.data_ptr(), _bytes(what, dev, plan),
+                                            err_word.data_ptr(), _stream_of(dev))
+    if rc:
+        raise PrismError(rc, what)
 
 
 def prism_op_attention_paged(q, k_cache, v_cache, block_table, plan, n_seq, max_q_len, n_q_heads, dtype, out, workspace, err_word,
                              impl=PRISM_IMPL_AUTO):
     what = "attention_paged"
-    _here(what, q, k_cache, v_cache, block_table, plan, out, workspace, err_word)
-    c = _cache(what, k_cache, v_cache, dtype)
-    s_q = _rows(what, q, dtype, n_q_heads * c.head_dim)
-    s_out = _rows(what, out, dtype, n_q_heads * c.head_dim)
-    _refuse_unless(out.shape[0] >= q.shape[0], what + ": a row of out for every row of q")
-    _ints(what, (err_word, 1))
-    stride = _table(what, block_table, n_seq)
-    _refuse_unless(plan.is_contiguous() and (workspace is None or workspace.is_contiguous()), what + ": plan and workspace")
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(_L().prism_op_attention_paged(_p(q), s_q, C.byref(c), _p(block_table), stride, block_table.shape[1], _p(plan),
-                                         plan.numel() * plan.element_size(), n_seq, q.shape[0], max_q_len, n_q_heads, impl,
-                                         _p(out), s_out, _p(workspace), ws_bytes, _p(err_word), _stream()), what)
+    dev = _device(what, err_word)
+    c = _cache(what, dev, k_cache, v_cache, dtype)
+    rows, width = q.shape[0], n_q_heads * c.head_dim
+    s_q, s_out = _matrix(what, dev, q, dtype, width), _matrix(what, dev, out, dtype, width, rows)
+    _ints(what, dev, (err_word, 1))
+    stride = _table(what, dev, block_table, n_seq)
+    rc = _L().prism_op_attention_paged(q.data_ptr(), s_q, c, block_table.data_ptr(), stride, block_table.shape[1], plan.data_ptr(),
+                                       _bytes(what, dev, plan), n_seq, rows, max_q_len, n_q_heads, impl, out.data_ptr(), s_out,
+                                       _p(workspace), 0 if workspace is None else _bytes(what, dev, workspace),
+                                       err_word.data_ptr(), _stream_of(dev))
+    if rc:
+        raise PrismError(rc, what)
 
 
 def prism_op_wait_selftest(limit_cycles, err_word):
