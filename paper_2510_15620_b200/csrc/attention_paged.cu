@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restri
     if (len < piece) len = (unsigned)min(piece, 0x7fffffffll);
     unsigned items_n = 0, parts_n = 0;
     for (int t = lane; t < n_tiles; t += 32) {
-      const unsigned k = s_keys[t], c = max(1u, (k + len - 1) / len);
+      const unsigned k = s_keys[t], c = (int)k > sh.min_cut ? max(1u, (k + len - 1) / len) : 1u;
       items_n += c;
       parts_n += c > 1 ? c : 0;
     }
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restri
     int len = 0;
     if (t >= 0) {
       r = tile_at(t);
-      const long long cuts = (r.keys + piece - 1) / piece;
+      const long long cuts = r.keys > sh.min_cut ? (r.keys + piece - 1) / piece : 1;
       if (cuts > 1) {
         len = (int)(((r.keys + cuts - 1) / cuts + sh.piece_unit - 1) / sh.piece_unit * sh.piece_unit);
         c.a = (r.keys + len - 1) / len;
@@ -275,161 +275,212 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedPlanHeader want, const 
 
 // ------------------------------------------------------------------------------------------------ CUDA-core kernel
 // fp32 (and bf16 at head sizes without a tensor-core kernel): R query rows against 64 keys at a time, 256 threads as a
-// 16 x 16 grid, each thread R/16 rows x 4 keys of the scores and R/16 rows x dh/16 columns of the output.  Keys and values
-// are widened to fp32 in shared memory; rows are padded by four floats so that the 16-byte reads of eight
-// neighbouring key rows fall into different banks.
+// 16 x 16 grid, each thread R/16 rows x 4 keys of the scores and R/16 rows x 4 NC columns of the output, both products fed by
+// 16-byte shared-memory reads (eight for 64 FMAs at R = 64).  Keys and values arrive by asynchronous copies in their own element
+// type: the values of a tile load under its scores, the next tile's keys under its second product, and the addresses (one
+// page-table read per key) are worked out a tile ahead.  Rows are padded by 16 bytes so that neighbouring rows start in
+// different banks.
+// Bound by FMA issue and shared-memory reads at R = 64, by latency in small calls, by reading the cache at R = 16.
 constexpr int kKeys = 64;
 
-__device__ __forceinline__ void store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
 __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
   const uint2 u = *reinterpret_cast<const uint2*>(p);
   return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                      __uint_as_float(u.y & 0xffff0000u));
 }
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
+  __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+}
+// 16 bytes to shared memory; zeros where there is nothing to read
+__device__ __forceinline__ void copy16(void* dst, const void* src, bool some) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
+               "r"(some ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+template <typename T>
 __host__ __device__ constexpr int simt_smem(int rows, int dh) {
-  return 4 * ((rows + 2 * kKeys) * (dh + 4) + rows * (kKeys + 4));
+  return (rows + 2 * kKeys) * (dh * (int)sizeof(T) + 16) + rows * (kKeys + 4) * 4 + 2 * kKeys * 8;
 }
 
-template <typename T, int R, int COLS>
+template <typename T, int R, int NC>
 __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, float scale_log2) {
   pdl_sync();
-  extern __shared__ __align__(16) float sm[];
+  extern __shared__ __align__(16) unsigned char smem[];
   constexpr int RT = R / 16;
   const PagedPlanHeader* hd = static_cast<const PagedPlanHeader*>(a.plan);
-  const int hkv = a.c.hkv, dh = a.c.dh, group = a.hq / hkv, ld = dh + 4;
+  const int hkv = a.c.hkv, dh = a.c.dh, group = a.hq / hkv;
+  // the grid is not larger than the list's room, so the first item can be fetched beside the header
+  PagedItem it = paged_item_raw(hd, blockIdx.x / hkv);
   if (hd->kind != kPagedSimt || hd->hq != a.hq || hd->hkv != hkv || hd->dh != dh || hd->total_q != a.total_q ||
       hd->n_seq != a.n_seq || hd->max_q != a.max_q || hd->rows != R) {
     if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(a.err, kErrBadOffsets);
     return;
   }
-  if (threadIdx.x == 0 && blockIdx.x == 0 && hd->n_items * hkv > (int)gridDim.x) atomicOr(a.err, kErrBadPage);
-  const int item = blockIdx.x / hkv, h = blockIdx.x % hkv;
-  if (item >= hd->n_items) return;
-  const PagedItem it = paged_item(hd, item, a.max_pages, shift, a.ws, a.err);
-  const int causal = hd->causal;
-  float* s_q = sm;
-  float* s_k = s_q + R * ld;
-  float* s_v = s_k + kKeys * ld;
-  float* s_p = s_v + kKeys * ld;
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, q4 = dh >> 2;
-  const T* q = static_cast<const T*>(a.q);
-  for (int u = tid; u < R * q4; u += 256) {
-    const int r = u / q4, c = (u % q4) * 4, tok = r / group;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (tok < it.n_tok) v = load4(q + (it.row0 + tok) * a.q_stride + (long long)(h * group + r % group) * dh + c);
-    *reinterpret_cast<float4*>(s_q + r * ld + c) = v;
-  }
-  // rows of this thread: ty + 16 i.  lim: keys below it are visible
-  int lim[RT];
-  float m[RT], l[RT], o[RT][COLS];
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    const int r = ty + 16 * i, tok = r / group;
-    lim[i] = tok < it.n_tok ? (causal ? min(it.k1, it.pos0 + tok + 1) : it.k1) : 0;
-    m[i] = -INFINITY, l[i] = 0.f;
-#pragma unroll
-    for (int c = 0; c < COLS; ++c) o[i][c] = 0.f;
-  }
-  const int* row = a.table + it.seq * a.table_stride;
-  for (int k0 = it.k0; k0 < it.k1; k0 += kKeys) {
-    __syncthreads();
-    for (int u = tid; u < kKeys * q4; u += 256) {
-      const int kk = u / q4, c = (u % q4) * 4, key = k0 + kk;
-      float4 kf = make_float4(0.f, 0.f, 0.f, 0.f), vf = kf;
+  const int total = hd->n_items * hkv, causal = hd->causal;
+  const int ld = dh + 16 / (int)sizeof(T);          // elements from row to row
+  const int pieces = dh * (int)sizeof(T) / 16;      // 16-byte pieces of a row
+  T* s_q = reinterpret_cast<T*>(smem);
+  T* s_k = s_q + R * ld;
+  T* s_v = s_k + kKeys * ld;
+  float* s_p = reinterpret_cast<float*>(s_v + kKeys * ld);
+  long long* s_at = reinterpret_cast<long long*>(s_p + R * (kKeys + 4));  // [2][64] element offset of each key's row, or -1
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  for (int work = blockIdx.x; work < total; work += gridDim.x) {
+    const int h = work % hkv;
+    if (work != (int)blockIdx.x) it = paged_item_raw(hd, work / hkv);
+    paged_item_check(it, a.max_pages, shift, a.ws, a.err);
+    const int* row = a.table + it.seq * a.table_stride;
+    // where the keys of tile t lie, by the first 64 threads
+    auto locate = [&](int t) {
+      if (tid >= kKeys) return;
+      const int key = it.k0 + t * kKeys + tid;
+      long long at = -1;
       if (key < it.k1) {
-        const int j = key >> shift, id = j < a.max_pages ? row[j] : -1;
-        if ((unsigned)id < (unsigned)a.c.num_pages) {
-          const long long at = id * a.c.page_stride + (((long long)h << shift) + (key & ((1 << shift) - 1))) * dh + c;
-          kf = load4(static_cast<const T*>(a.c.k) + at);
-          vf = load4(static_cast<const T*>(a.c.v) + at);
-        } else if (c == 0) {
+        const int id = row[key >> shift];  // key < k1 <= max_pages << shift
+        if ((unsigned)id < (unsigned)a.c.num_pages)
+          at = id * a.c.page_stride + (((long long)h << shift) + (key & ((1 << shift) - 1))) * dh;
+        else
           atomicOr(a.err, kErrBadPage);
-        }
       }
-      *reinterpret_cast<float4*>(s_k + kk * ld + c) = kf;
-      *reinterpret_cast<float4*>(s_v + kk * ld + c) = vf;
+      s_at[(t & 1) * kKeys + tid] = at;
+    };
+    auto fetch = [&](T* dst, const void* src, int t) {
+      const long long* at = s_at + (t & 1) * kKeys;
+      for (int u = tid; u < kKeys * pieces; u += 256) {
+        const int kk = u / pieces, c = (u % pieces) * (16 / (int)sizeof(T));
+        const long long o = at[kk];
+        copy16(dst + kk * ld + c, static_cast<const T*>(src) + (o < 0 ? 0 : o + c), o >= 0);
+      }
+      copies_commit();
+    };
+    const int n_tiles = it.k1 > it.k0 ? (it.k1 - it.k0 + kKeys - 1) / kKeys : 0;
+    __syncthreads();  // the previous item's shared memory has been read
+    const T* q = static_cast<const T*>(a.q);
+    for (int u = tid; u < R * pieces; u += 256) {
+      const int r = u / pieces, c = (u % pieces) * (16 / (int)sizeof(T)), tok = r / group;
+      const bool some = tok < it.n_tok;
+      copy16(s_q + r * ld + c, some ? q + (it.row0 + tok) * a.q_stride + (long long)(h * group + r % group) * dh + c : q, some);
     }
+    locate(0);
     __syncthreads();
-    float s[RT][4];
+    if (n_tiles > 0) fetch(s_k, a.c.k, 0);  // one group with the queries
+    // rows of this thread: ty + 16 i.  lim: keys below it are visible
+    int lim[RT];
+    float m[RT], l[RT];
+    float4 o[RT][NC];
 #pragma unroll
-    for (int i = 0; i < RT; ++i)
+    for (int i = 0; i < RT; ++i) {
+      const int r = ty + 16 * i, tok = r / group;
+      lim[i] = tok < it.n_tok ? (causal ? min(it.k1, it.pos0 + tok + 1) : it.k1) : 0;
+      m[i] = -INFINITY, l[i] = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
-#pragma unroll 4
-    for (int c = 0; c < dh; c += 4) {
-      float4 qa[RT], kb[4];
-#pragma unroll
-      for (int i = 0; i < RT; ++i) qa[i] = *reinterpret_cast<const float4*>(s_q + (ty + 16 * i) * ld + c);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) kb[j] = *reinterpret_cast<const float4*>(s_k + (tx + 16 * j) * ld + c);
+      for (int c = 0; c < NC; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int t = 0; t < n_tiles; ++t) {
+      const int k0 = it.k0 + t * kKeys;
+      if (t > 0) __syncthreads();  // every thread is through with the previous tile's values
+      fetch(s_v, a.c.v, t);
+      if (t + 1 < n_tiles) locate(t + 1);
+      copies_wait<1>();  // keys (and queries); the values are still on their way
+      __syncthreads();
+      float s[RT][4];
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          s[i][j] += qa[i].x * kb[j].x + qa[i].y * kb[j].y + qa[i].z * kb[j].z + qa[i].w * kb[j].w;
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+      for (int c = 0; c < dh; c += 4) {
+        float4 qa[RT], kb[4];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) qa[i] = load4(s_q + (ty + 16 * i) * ld + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) kb[j] = load4(s_k + (tx + 16 * j) * ld + c);
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            s[i][j] += qa[i].x * kb[j].x + qa[i].y * kb[j].y + qa[i].z * kb[j].z + qa[i].w * kb[j].w;
+      }
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[i][j] = k0 + tx + 16 * j < lim[i] ? s[i][j] * scale_log2 : -INFINITY;
+          mx = fmaxf(mx, s[i][j]);
+        }
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.f : mn;
+        const float f = exp2f(m[i] - ref);
+        m[i] = mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = exp2f(s[i][j] - ref);
+          sum += p;
+          s_p[(ty + 16 * i) * (kKeys + 4) + tx + 16 * j] = p;
+        }
+        l[i] = l[i] * f + sum;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[i][c].x *= f, o[i][c].y *= f, o[i][c].z *= f, o[i][c].w *= f;
+      }
+      copies_wait<0>();
+      __syncthreads();  // the values are there, the keys have been read, the next tile's addresses are known
+      if (t + 1 < n_tiles) fetch(s_k, a.c.k, t + 1);
+      const int nk = min(kKeys, it.k1 - k0);
+      for (int kk = 0; kk < nk; kk += 4) {  // (keys of the last four beyond nk have p = 0 and zero values)
+        float4 p[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) p[i] = *reinterpret_cast<const float4*>(s_p + (ty + 16 * i) * (kKeys + 4) + kk);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int col = tx * 4 + 64 * c;
+          if (col < dh) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float4 v = load4(s_v + (kk + e) * ld + col);
+#pragma unroll
+              for (int i = 0; i < RT; ++i) {
+                const float w = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
+                o[i][c].x += w * v.x, o[i][c].y += w * v.y, o[i][c].z += w * v.z, o[i][c].w += w * v.w;
+              }
+            }
+          }
+        }
+      }
     }
+    copies_wait<0>();
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-      float mx = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        s[i][j] = k0 + tx + 16 * j < lim[i] ? s[i][j] * scale_log2 : -INFINITY;
-        mx = fmaxf(mx, s[i][j]);
-      }
-#pragma unroll
-      for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-      const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.f : mn;
-      const float f = exp2f(m[i] - ref);
-      m[i] = mn;
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float p = exp2f(s[i][j] - ref);
-        sum += p;
-        s_p[(ty + 16 * i) * (kKeys + 4) + tx + 16 * j] = p;
-      }
-      l[i] = l[i] * f + sum;
-#pragma unroll
-      for (int c = 0; c < COLS; ++c) o[i][c] *= f;
-    }
-    __syncwarp();  // a row's sixteen threads are half a warp
-    const int nk = min(kKeys, it.k1 - k0);
-    for (int kk = 0; kk < nk; ++kk) {
-      float p[RT];
-#pragma unroll
-      for (int i = 0; i < RT; ++i) p[i] = s_p[(ty + 16 * i) * (kKeys + 4) + kk];
-#pragma unroll
-      for (int c = 0; c < COLS; ++c) {
-        const float v = tx + 16 * c < dh ? s_v[kk * ld + tx + 16 * c] : 0.f;
-#pragma unroll
-        for (int i = 0; i < RT; ++i) o[i][c] += p[i] * v;
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-#pragma unroll
-    for (int d = 8; d > 0; d >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
-    const int r = ty + 16 * i, tok = r / group;
-    if (tok >= it.n_tok) continue;
-    if (it.part < 0) {
+      for (int d = 8; d > 0; d >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+      const int r = ty + 16 * i, tok = r / group;
+      if (tok >= it.n_tok) continue;
+      float* p = it.part < 0 ? nullptr : a.ws + ((long long)it.part * hkv + h) * paged_part_floats(R, dh);
       const bool any = lim[i] > it.k0;
       const float inv = 1.f / l[i];
       T* dst = static_cast<T*>(a.out) + (it.row0 + tok) * a.out_stride + (long long)(h * group + r % group) * dh;
 #pragma unroll
-      for (int c = 0; c < COLS; ++c)
-        if (tx + 16 * c < dh) store(dst + tx + 16 * c, any ? o[i][c] * inv : 0.f);
-    } else {
-      float* p = a.ws + ((long long)it.part * hkv + h) * paged_part_floats(R, dh);
-#pragma unroll
-      for (int c = 0; c < COLS; ++c) {
-        const int col = tx + 16 * c;
-        if (col < dh) p[((long long)(col >> 2) * R + r) * 4 + (col & 3)] = o[i][c];
+      for (int c = 0; c < NC; ++c) {
+        const int col = tx * 4 + 64 * c;
+        float4 v = o[i][c];
+        if (col >= dh) continue;
+        if (p) {
+          *reinterpret_cast<float4*>(p + ((long long)(col >> 2) * R + r) * 4) = v;
+        } else {
+          v = any ? make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
+          store4(dst + col, v);
+        }
       }
-      if (tx == 0) *reinterpret_cast<float2*>(p + (long long)R * dh + 2 * r) = make_float2(m[i], l[i]);
+      if (p && tx == 0) *reinterpret_cast<float2*>(p + (long long)R * dh + 2 * r) = make_float2(m[i], l[i]);
     }
   }
 }
@@ -440,24 +491,29 @@ int log2_of(int x) {
   return s;
 }
 
-template <typename T, int R, int COLS>
+template <typename T, int R, int NC>
 cudaError_t simt_launch(const PagedAttnArgs& a, int grid, cudaStream_t st) {
   static std::atomic<unsigned long long> set;
-  const int smem = simt_smem(R, a.c.dh);
-  if (cudaError_t e = ensure_dynamic_smem(k_paged_simt<T, R, COLS>, simt_smem(R, 16 * COLS), set)) return e;
+  const int smem = simt_smem<T>(R, a.c.dh);
+  if (cudaError_t e = ensure_dynamic_smem(k_paged_simt<T, R, NC>, simt_smem<T>(R, 64 * NC), set)) return e;
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)a.c.dh);
-  k_paged_simt<T, R, COLS><<<grid, 256, smem, st>>>(a, log2_of(a.c.page_size), scale_log2);
+  k_paged_simt<T, R, NC><<<grid, 256, smem, st>>>(a, log2_of(a.c.page_size), scale_log2);
   return cudaGetLastError();
 }
+static_assert(simt_smem<float>(64, 256) <= 232448, "exceeds the shared memory one block may have");
 
 }  // namespace
 
-bool paged_plan_shape(int max_q, int hq, int hkv, int dh, int dtype, int impl, PagedPlanShape* s) {
+bool paged_plan_shape(int n_seq, int total_q, int max_q, int hq, int hkv, int dh, int dtype, int impl, PagedPlanShape* s) {
   const int g = hq / hkv;
   if (max_q < 1) max_q = 1;
   s->group = g;
   s->piece_unit = 128;
   s->target = 148 * 8;
+  // Cutting costs a join, so it has to be worth 2 us at least: where every SM has a block anyway that is a tile of 2048 keys.
+  // Tables no wider than min_cut also save the join's launch.
+  const bool busy = (long long)n_seq * hkv >= 148;
+  s->min_cut = busy ? 2048 : 512;
   const bool few = (long long)max_q * g <= 16;
   if (dtype == 1 && impl == 0 && (dh == 64 || dh == 128) && g <= 128) {
     if (few) {
@@ -472,8 +528,10 @@ bool paged_plan_shape(int max_q, int hq, int hkv, int dh, int dtype, int impl, P
     return true;
   }
   if (g > 64) return false;
-  s->kind = kPagedSimt, s->rows = few ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 256, s->slots = 148 * 2;
-  s->ns_key = few ? 10.f : 40.f, s->ns_key_block = 0.f, s->ns_item = 2000.f, s->ns_part = 1000.f, s->ns_join = 2500.f;
+  // 64 rows a block use the FMA units best (16 are bound by shared-memory reads); 16 spread a small call over the SMs
+  const bool small = few || (g <= 16 && ((long long)total_q * g / 64 + n_seq) * hkv < 148 * 2);
+  s->kind = kPagedSimt, s->rows = small ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 256, s->slots = 148 * 2;
+  s->ns_key = small ? 10.f : 40.f, s->ns_key_block = 0.f, s->ns_item = 2000.f, s->ns_part = 1000.f, s->ns_join = 2500.f;
   return true;
 }
 
@@ -516,12 +574,12 @@ cudaError_t launch_paged_join(const PagedAttnArgs& a, const PagedPlanShape& s, i
 cudaError_t launch_paged_simt(const PagedAttnArgs& a, const PagedPlanShape& s, int grid, cudaStream_t st) {
   const int dh = a.c.dh;
 #define PRISM_SIMT(T)                                                                     \
-  (s.rows == 16 ? (dh <= 64    ? simt_launch<T, 16, 4>(a, grid, st)                       \
-                   : dh <= 128 ? simt_launch<T, 16, 8>(a, grid, st)                       \
-                               : simt_launch<T, 16, 16>(a, grid, st))                     \
-                : (dh <= 64    ? simt_launch<T, 64, 4>(a, grid, st)                       \
-                   : dh <= 128 ? simt_launch<T, 64, 8>(a, grid, st)                       \
-                               : simt_launch<T, 64, 16>(a, grid, st)))
+  (s.rows == 16 ? (dh <= 64    ? simt_launch<T, 16, 1>(a, grid, st)                       \
+                   : dh <= 128 ? simt_launch<T, 16, 2>(a, grid, st)                       \
+                               : simt_launch<T, 16, 4>(a, grid, st))                      \
+                : (dh <= 64    ? simt_launch<T, 64, 1>(a, grid, st)                       \
+                   : dh <= 128 ? simt_launch<T, 64, 2>(a, grid, st)                       \
+                               : simt_launch<T, 64, 4>(a, grid, st)))
   return a.c.dtype == 1 ? PRISM_SIMT(__nv_bfloat16) : PRISM_SIMT(float);
 #undef PRISM_SIMT
 }

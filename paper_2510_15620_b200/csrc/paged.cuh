@@ -31,6 +31,7 @@ struct PagedPlanShape {
   int rows;        // query rows (token, head of the group) an item has room for
   int tokens;      // tokens an item covers
   int min_piece;   // keys: tiles are never cut into pieces shorter than this
+  int min_cut;     // keys: shorter tiles are not cut at all
   int piece_unit;  // keys: pieces are multiples of this
   int target;      // pieces are at least total keys * hkv / target long
   int slots;       // blocks that run at a time
@@ -82,7 +83,7 @@ struct PagedJoin {
 static_assert(sizeof(PagedPlanHeader) == 64 && sizeof(PagedItem) == 32 && sizeof(PagedJoin) == 32, "plan layout");
 
 // Returns false where no kernel serves the shape.
-bool paged_plan_shape(int max_q, int hq, int hkv, int dh, int dtype, int impl, PagedPlanShape* s);
+bool paged_plan_shape(int n_seq, int total_q, int max_q, int hq, int hkv, int dh, int dtype, int impl, PagedPlanShape* s);
 
 // Upper bounds the buffers are sized by (the lengths live on the device).  An item covers s.tokens tokens of one
 // sequence, so there are at most total_q / tokens + n_seq tiles; pieces are at least total keys * hkv / target long, so

@@ -41,7 +41,7 @@ int check_shape(int32_t n_seq, int32_t total_q, int32_t max_q_len, int32_t hq, i
   if (impl != PRISM_IMPL_AUTO && impl != PRISM_IMPL_SIMT) return PRISM_ERR_UNSUPPORTED;
   if (n_seq > PRISM_MAX_CANDIDATES) return PRISM_ERR_SHAPE_LIMIT;
   if (dh < 16 || dh > 256 || dh % 16 || hkv > 1024) return PRISM_ERR_UNSUPPORTED;
-  if (!paged_plan_shape(max_q_len, hq, hkv, dh, dtype, impl, s)) return PRISM_ERR_UNSUPPORTED;
+  if (!paged_plan_shape(n_seq, total_q, max_q_len, hq, hkv, dh, dtype, impl, s)) return PRISM_ERR_UNSUPPORTED;
   // rows of the work list and of the grid are counted in 32 bits
   if (paged_plan_bounds(*s, hkv, n_seq, total_q).items * hkv > INT32_MAX) return PRISM_ERR_SHAPE_LIMIT;
   return PRISM_OK;
@@ -137,9 +137,9 @@ int prism_op_attention_paged(const void* q, int64_t q_stride, const prism_kv_cac
     return PRISM_ERR_INVALID_ARG;
   const PagedPlanBounds bound = paged_plan_bounds(s, hkv, n_seq, total_q);
   if (!plan || !aligned16(plan) || plan_bytes < paged_plan_bytes(bound)) return PRISM_ERR_INVALID_ARG;
-  // A tile is cut only if its keys, which the table's width bounds, are more than the shortest piece.
+  // A tile is cut only if it has more keys than min_cut, and the table's width bounds its keys.
   const int64_t max_keys = (int64_t)max_pages * cache->page_size;
-  const bool may_cut = max_keys > s.min_piece;
+  const bool may_cut = max_keys > s.min_cut;
   if (may_cut && (!workspace || !aligned16(workspace) || workspace_bytes < paged_ws_bytes(s, bound, hkv, dh))) return PRISM_ERR_INVALID_ARG;
   if (n_seq == 0 || total_q == 0 || max_q_len == 0) return PRISM_OK;
   if (!q || !out || !aligned16(q) || !aligned16(out) || (max_pages > 0 && !block_table)) return PRISM_ERR_INVALID_ARG;
@@ -147,8 +147,11 @@ int prism_op_attention_paged(const void* q, int64_t q_stride, const prism_kv_cac
   a.q = q, a.q_stride = q_stride, a.c = view(cache), a.table = block_table, a.max_pages = max_pages, a.table_stride = table_stride;
   a.plan = plan, a.n_seq = n_seq, a.total_q = total_q, a.max_q = max_q_len, a.hq = n_q_heads, a.out = out, a.out_stride = out_stride;
   a.ws = may_cut ? static_cast<float*>(workspace) : nullptr, a.err = err_word;
-  const int64_t tiles = (int64_t)total_q / s.tokens + n_seq;
-  const int grid = (int)((may_cut ? bound.items : tiles) * hkv);
+  // One block per uncut item.  Pieces beyond that are second helpings of the same blocks, but there are at least as many blocks
+  // as run at a time; the tcgen05 kernel takes a block per possible piece (they are handed out by the work distributor).
+  const int64_t tiles = ((int64_t)total_q / s.tokens + n_seq) * hkv, all = bound.items * hkv;
+  const int64_t some = tiles > s.slots ? tiles : s.slots;
+  const int grid = (int)(!may_cut ? tiles : s.kind == kPagedTiles || all < some ? all : some);
   cudaError_t e = s.kind == kPagedTokens  ? launch_paged_tokens(a, s, grid, S(stream))
                   : s.kind == kPagedTiles ? launch_paged_tiles(a, s, grid, S(stream))
                                           : launch_paged_simt(a, s, grid, S(stream));

@@ -121,7 +121,7 @@ def plan(L, p, **kw):
 
 def attn(L, p, c=None, **kw):
     c = cache(p) if c is None else c
-    d = dict(q=p, s_q=256, c=C.byref(c) if c != 0 else None, table=p, stride=32, max_pages=32, plan=p, plan_bytes=1 << 30, n=4, total=8, max_q=2, hq=4,
+    d = dict(q=p, s_q=256, c=C.byref(c) if c != 0 else None, table=p, stride=64, max_pages=64, plan=p, plan_bytes=1 << 30, n=4, total=8, max_q=2, hq=4,
              impl=0, out=p, s_out=256, ws=p, ws_bytes=1 << 40, err=p)
     d.update(kw)
     return L.prism_op_attention_paged(*d.values(), None)
@@ -139,7 +139,7 @@ def test_attention_refuses(L, buf):
         assert attn(L, p, **kw) == OK, kw                # nothing to do: nothing is launched
     for kw in (dict(q=None), dict(out=None), dict(table=None), dict(plan=None), dict(err=None), dict(ws=None), dict(c=0),
                dict(q=p + 8), dict(out=p + 4), dict(plan=p + 4), dict(ws=p + 8), dict(plan_bytes=need_plan - 1),
-               dict(ws_bytes=need_ws - 1), dict(s_q=248), dict(s_q=260), dict(s_out=252), dict(stride=31), dict(max_pages=-1),
+               dict(ws_bytes=need_ws - 1), dict(s_q=248), dict(s_q=260), dict(s_out=252), dict(stride=63), dict(max_pages=-1),
                dict(max_pages=1 << 27, stride=1 << 27), dict(hq=5), dict(n=-1)):
         assert attn(L, p, **kw) == INVALID, kw
     assert attn(L, p, impl=3) == UNSUPPORTED
