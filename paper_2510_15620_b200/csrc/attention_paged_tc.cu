@@ -22,14 +22,18 @@
 // Tensor memory: S_A, S_B, O_A, O_B.  P_x(g) overlies S_x(g).  Rows that no token owns are not computed; a warp without any
 // live row only keeps the barriers' phases.
 //
-// What bounds it: the chain softmax -> P V -> next scores of each tile (2430 + 1330 cycles a block, clock64), which the other
-// tile covers to two thirds; tensor core and special-function unit are 55-60 % busy.  Measured steps (us; 2368 tokens behind
-// 16 k / 1024 behind 64 k / 100 documents of 320 behind 512): two threads per row that meet once a block 625 / 1066 / 284; one
-// thread per row, P V in halves 618 / 1093 / 279; MMAs issued by an elected thread instead of lane 0 (38 instead of 60 issue
-// cycles an instruction, which beside eight softmax warps decides who waits) 611 / 1074 / 255; the issuing warp in step
-// 608 / 1070 / 250; exponentials shared with the FMA pipe 568 / 1039 / 250.  Tried and not kept: two threads per row with one
-// deciding the reference for both 650 / 1120 / 286; whole rows in 208 registers (register reallocation) 638 / 1107 / 261;
-// scores double-buffered in blocks of 64 keys 614 / 1103 / 250; suspended instead of polled waits 675 / 1151 / 264.
+// What bounds it: the chain softmax -> P V -> next scores of each tile (about 2400 + 1330 cycles a block, clock64), which the
+// other tile covers to two thirds; tensor core and special-function unit are 55-60 % busy.  In short sequences the change from
+// unit to unit counts (Q, first scores and output, some 3000 cycles), and so does code size: three roles with long unrolled
+// bodies evict each other from the instruction caches, so every body exists once.
+// Measured steps (us; 2368 tokens behind 16 k / 1024 behind 64 k / 100 documents of 128-512 behind 512; 32, 32 and 16 query
+// heads): two threads per row that meet once a block 625 / 1066 / 288; one thread per row, P V in halves 618 / 1093 / 279; MMAs
+// issued by an elected thread instead of lane 0 (38 instead of 60 issue cycles an instruction) 611 / 1074 / 255; the issuing warp
+// in step 608 / 1070 / 254; exponentials shared with the FMA pipe 570 / 1040 / 254; output rows of 128 bytes 562 / 1017 / 247; one
+// copy of the softmax step, re-entered when a reference moves, and of the issuing step 566 / 1020 / 228.
+// Tried and not kept: two threads per row, one deciding the reference for both 650 / 1120 / 286; whole rows in 208 registers
+// (register reallocation) 638 / 1107 / 261; scores double-buffered in blocks of 64 keys 614 / 1103 / 250, again with one copy of
+// the code 709 / 1179 / 279; suspended instead of polled waits 675 / 1151 / 264; the output step unrolled 561 / 1000 / 268.
 // Values behind the last key of a piece (stale rows of the last page) are cleared in shared memory before the second
 // product, so that nothing a page happens to hold meets a zero probability.
 // Rounding: probabilities become bf16 for the second product; sums, references and outputs stay fp32 until the one
@@ -46,7 +50,7 @@ using namespace tc;
 
 constexpr int BM = 128, BN = 128;
 constexpr int NK = 2, NV = 2;
-constexpr int kStageBytes = 32 * 64;  // per softmax warp: 32 rows x 32 bf16 of output on their way to global memory
+constexpr int kStageBytes = 32 * 128;  // per softmax warp: 32 rows x 64 bf16 of output on their way to global memory
 constexpr int kBarBytes = 512;
 __host__ __device__ constexpr int tile_bytes(int dh) { return 128 * dh * 2; }
 __host__ __device__ constexpr int smem_bytes(int dh) {
@@ -63,13 +67,12 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+               : "memory");
 }
 // The wait names the loaded registers, so that nothing that uses them can move in front of it.
 __device__ __forceinline__ void tmem_ld_wait32(uint32_t* r) {
@@ -174,11 +177,14 @@ struct UnitReader {
     ring = ring_, b_full = b_full_, b_empty = b_empty_, n = 0, n_blocks = 0, n_tok = 0;
   }
   // Moves to the next unit (whole warps only); false at the end of the work or when the wait gave up.
-  template <bool kWarp>
+  template <bool kUniform>
   __device__ __forceinline__ bool next(int* err, volatile int* abort_flag) {
     if (!warp_wait(b_full + 8 * (n % NI), (n / NI) & 1, err, abort_flag)) return false;
-    n_blocks = __shfl_sync(0xffffffffu, ring[n % NI].n_blocks, 0);  // the same in every lane, and known to be
-    n_tok = __shfl_sync(0xffffffffu, ring[n % NI].n_tok, 0);
+    n_blocks = ring[n % NI].n_blocks, n_tok = ring[n % NI].n_tok;
+    if (kUniform) {  // the same in every lane, and known to be
+      n_blocks = __shfl_sync(0xffffffffu, n_blocks, 0);
+      n_tok = __shfl_sync(0xffffffffu, n_tok, 0);
+    }
     return n_blocks > 0;
   }
   __device__ __forceinline__ volatile Unit& rec() { return ring[n % NI]; }
@@ -438,17 +444,15 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       ++pc;
       return true;
     };
-    if (s_has) {
-      const bool two = its.n_tok > tpt;
-      ok = issue_s(0, !two, sq0);
-      if (ok && two) ok = issue_s(1, true, sq1);
-    }
-    while (ok && p_has) {
-      const bool p_two = itp.n_tok > tpt, s_now = s_has, s_two = s_now && its.n_tok > tpt;
-      ok = issue_pv(0, !p_two, pc0);
+    // The first round issues the first scores only (one loop, so that the code of a step exists once: the roles' code together
+    // is larger than the instruction caches like).
+    for (bool first = true; ok && p_has; first = false) {
+      const bool p_two = !first && itp.n_tok > tpt, s_now = s_has, s_two = s_now && its.n_tok > tpt;
+      if (!first) ok = issue_pv(0, !p_two, pc0);
       if (ok && s_now) ok = issue_s(0, !s_two, sq0);
       if (ok && p_two) ok = issue_pv(1, true, pc1);
       if (ok && s_two) ok = issue_s(1, true, sq1);
+      if (first) continue;
       ++vc;
       if (++pj == itp.n_blocks) {
         pj = 0;
@@ -475,7 +479,7 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
     it.init(ring, b_unit_full, b_unit_empty);
     uint32_t gc = 0;  // blocks of this tile handled so far
     bool ok = true;
-    while (ok && it.next<true>(err, abort_flag)) {
+    while (ok && it.next<false>(err, abort_flag)) {
       const int n_tok = x == 0 ? min(it.n_tok, tpt) : it.n_tok - tpt;  // tokens of this tile
       if (n_tok <= 0) {  // B of a unit that has A only
         __syncwarp();
@@ -525,7 +529,7 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             if (key + 32 > lim_min) {
 #pragma unroll
               for (int e = 0; e < 32; ++e)
-                if (key + e >= lim) cur[e] = 0xff800000u;  // -inf
+                if (e >= lim - key) cur[e] = 0xff800000u;  // -inf
             }
             float sum;
             exp_chunk(cur, sc2, ms, out16, sum);
@@ -534,28 +538,29 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           tmem_ld32(t_s, buf[0]);
           tmem_ld_wait32(buf[0]);
           if (j == 0) ms = sees ? __uint_as_float(buf[0][0]) * scale_log2 : 0.f;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (i == 1) tmem_ld_wait32(buf[0]);
-            tmem_ld32(t_s + (2 * i + 1) * 32, buf[1]);
+          bool moved = false;  // this half is being done again, with a new reference
+#pragma unroll 1
+          for (int i = 0; i < 2;) {
+            tmem_ld_wait32(buf[0]);
+            tmem_ld32(t_s + i * 64 + 32, buf[1]);
             float sum = chunk(2 * i, buf[0], pk);
             tmem_ld_wait32(buf[1]);
             if (i == 0) tmem_ld32(t_s + 64, buf[0]);
             sum += chunk(2 * i + 1, buf[1], pk + 16);
-            if (__any_sync(0xffffffffu, live && !(sum <= kBigSum))) {
+            if (!moved && __any_sync(0xffffffffu, live && !(sum <= kBigSum))) {
               // Rare: rows whose largest exponent is beyond 2^64 move their reference up by d = ceil(that exponent); what was
               // accumulated under the old one is scaled by 2^-d (exact).  This half's P has not been stored, so its scores
               // are still there; the other half's product, if it was issued, has to be in O first.
               if (i == 0) tmem_ld_wait32(buf[0]);
               float xmax = -INFINITY;
 #pragma unroll 1
-              for (int v = 0; v < 4; ++v) {
-                uint32_t o[16];
-                tmem_ld16(t_s + i * 64 + v * 16, o);
+              for (int v = 0; v < 64; v += 4) {
+                uint32_t o[4];
+                tmem_ld4(t_s + i * 64 + v, o);
                 tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                  if (kb + i * 64 + v * 16 + e < lim) xmax = fmaxf(xmax, fmaf(__uint_as_float(o[e]), scale_log2, -ms));
+                for (int e = 0; e < 4; ++e)
+                  if (kb + i * 64 + v + e < lim) xmax = fmaxf(xmax, fmaf(__uint_as_float(o[e]), scale_log2, -ms));
               }
               const float d = xmax > 64.f ? ceilf(xmax) : 0.f;
               const float f = exp2f(-d);
@@ -565,32 +570,30 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               }
               if (j > 0 || i == 1) {
 #pragma unroll 1
-                for (int v = 0; v < DH / 16; ++v) {
-                  uint32_t o[16];
-                  tmem_ld16(t_o + v * 16, o);
+                for (int v = 0; v < DH; v += 4) {
+                  uint32_t o[4];
+                  tmem_ld4(t_o + v, o);
                   tmem_ld_wait();
 #pragma unroll
-                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                  tmem_st16(t_o + v * 16, o);
+                  for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                  tmem_st4(t_o + v, o);
                 }
                 tmem_st_wait();
               }
               l *= f;
               ms += d;
-              tmem_ld32(t_s + 2 * i * 32, buf[0]);
-              tmem_ld_wait32(buf[0]);
-              sum = chunk(2 * i, buf[0], pk);
-              tmem_ld32(t_s + (2 * i + 1) * 32, buf[1]);
-              tmem_ld_wait32(buf[1]);
-              sum += chunk(2 * i + 1, buf[1], pk + 16);
-              if (i == 0) tmem_ld32(t_s + 64, buf[0]);
+              tmem_ld32(t_s + i * 64, buf[0]);
+              moved = true;
+              continue;
             }
+            moved = false;
             l += sum;
             tmem_st32(t_s + i * 32, pk);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive((i == 0 ? b_p1 : b_p2) + 8 * x);
+            ++i;
           }
           if (!ok) break;
         } else {
@@ -608,38 +611,39 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       tc_fence_after();
       if (warp_live) {
         if (part < 0) {
-          // This row's O_x / l as bf16, 32 columns at a time through the warp's staging rows (64 bytes each, 16-byte
-          // pieces XOR-swizzled), so that global stores are 64 contiguous bytes per row.
-          const float inv = 1.f / l;
-          const long long at = live ? (long long)(row0 + x * tpt + tt) * a.out_stride + (long long)(h * group + head) * DH : -1;
-          __nv_bfloat16* ocol = static_cast<__nv_bfloat16*>(a.out);
+          // This row's O_x / l as bf16, 64 columns at a time through the warp's staging rows (128 bytes each, 16-byte pieces
+          // XOR-swizzled), so that global stores are 128 contiguous bytes per row.
+          const float inv = sees ? 1.f / l : 0.f;
+          const int mine = live ? tt * 128 + head : -1;  // head < group <= 128
+          __nv_bfloat16* const ocol = static_cast<__nv_bfloat16*>(a.out) + (long long)(row0 + x * tpt) * a.out_stride +
+                                      (long long)h * group * DH + (lane & 7) * 8;
 #pragma unroll 1
-          for (int pt = 0; pt < DH / 32; ++pt) {
-            uint32_t o[32];
-            tmem_ld32(t_o + pt * 32, o);
+          for (int pt = 0; pt < DH / 64; ++pt) {
+            uint32_t o[64];
+            tmem_ld32(t_o + pt * 64, o);
+            tmem_ld32(t_o + pt * 64 + 32, o + 32);
             tmem_ld_wait32(o);
+            tmem_ld_wait32(o + 32);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const uint32_t dst = stg + lane * 64 + ((v ^ ((lane >> 1) & 3)) << 4);
+            for (int v = 0; v < 8; ++v) {
+              const uint32_t dst = stg + lane * 128 + ((v ^ (lane & 7)) << 4);
               uint32_t w4[4];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
+              for (int e = 0; e < 4; ++e)
                 w4[e] = pack_bf16(__uint_as_float(o[v * 8 + 2 * e]) * inv, __uint_as_float(o[v * 8 + 2 * e + 1]) * inv);
-                if (!sees) w4[e] = 0u;  // no visible key: zero
-              }
               asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w4[0]), "r"(w4[1]), "r"(w4[2]), "r"(w4[3])
                            : "memory");
             }
             __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int rr = i * 8 + (lane >> 2), chn = lane & 3;
+#pragma unroll 2
+            for (int i = 0; i < 8; ++i) {
+              const int rr = i * 4 + (lane >> 3);
               uint4 val;
               asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                            : "=r"(val.x), "=r"(val.y), "=r"(val.z), "=r"(val.w)
-                           : "r"(stg + rr * 64 + ((chn ^ ((rr >> 1) & 3)) << 4)));
-              const long long to = __shfl_sync(0xffffffffu, at, rr);
-              if (to >= 0) *reinterpret_cast<uint4*>(ocol + to + pt * 32 + chn * 8) = val;
+                           : "r"(stg + rr * 128 + (((lane & 7) ^ (rr & 7)) << 4)));
+              const int to = __shfl_sync(0xffffffffu, mine, rr);
+              if (to >= 0) *reinterpret_cast<uint4*>(ocol + (to >> 7) * a.out_stride + (to & 127) * DH + pt * 64) = val;
             }
             __syncwarp();
           }

@@ -177,10 +177,13 @@ def _stream_of(dev):
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
+_INTS = ": int32 tensors on the current device, contiguous and long enough"
+
+
 def _ints(what, dev, *pairs):
     for t, n in pairs:
         if t.dtype is not _I32 or t.get_device() != dev or not t.is_contiguous() or t.numel() < n:
-            raise PrismError(-1, what + ": int32 tensors on the current device, contiguous and long enough")
+            raise PrismError(-1, what + _INTS)
 
 
 def _row_stride(t):
@@ -222,8 +225,17 @@ def prism_op_page_append(len_new, kv_len_in, kv_len_out, page_size, num_pages, b
                          cu_q, pos, slot_map, err_word):
     what = "page_append"
     n, total, dev = len_new.numel(), slot_map.numel(), _device(what, err_word)
-    _ints(what, dev, (len_new, n), (kv_len_in, n), (kv_len_out, n), (free_pages, num_pages), (n_free_in, 1), (n_free_out, 1),
-          (cu_q, n + 1), (pos, total), (slot_map, total), (err_word, 1))
+    # (written out: a loop over the ten tensors takes twice as long)
+    if not (len_new.dtype is kv_len_in.dtype is kv_len_out.dtype is free_pages.dtype is n_free_in.dtype is n_free_out.dtype is
+            cu_q.dtype is pos.dtype is slot_map.dtype is err_word.dtype is _I32 and
+            len_new.get_device() == kv_len_in.get_device() == kv_len_out.get_device() == free_pages.get_device() ==
+            n_free_in.get_device() == n_free_out.get_device() == cu_q.get_device() == pos.get_device() ==
+            slot_map.get_device() == dev and
+            len_new.is_contiguous() and kv_len_in.is_contiguous() and kv_len_out.is_contiguous() and
+            free_pages.is_contiguous() and cu_q.is_contiguous() and pos.is_contiguous() and slot_map.is_contiguous() and
+            kv_len_in.numel() >= n and kv_len_out.numel() >= n and free_pages.numel() >= num_pages and n_free_in.numel() >= 1 and
+            n_free_out.numel() >= 1 and cu_q.numel() > n and pos.numel() >= total and err_word.numel() >= 1):
+        raise PrismError(-1, what + _INTS)
     stride = _table(what, dev, block_table, n)
     rc = _L().prism_op_page_append(len_new.data_ptr(), kv_len_in.data_ptr(), kv_len_out.data_ptr(), n, page_size, num_pages,
                                    block_table.shape[1], stride, block_table.data_ptr(), free_pages.data_ptr(),
@@ -238,8 +250,14 @@ def prism_op_page_release(old_of_new, kv_len_in, kv_len_out, page_size, num_page
     """n_new: survivors (default: all of old_of_new, which may be a longer buffer)."""
     what = "page_release"
     n, n_new, dev = kv_len_in.numel(), old_of_new.numel() if n_new is None else n_new, _device(what, err_word)
-    _ints(what, dev, (old_of_new, n_new), (kv_len_in, n), (kv_len_out, n), (free_pages, num_pages), (n_free_in, 1), (n_free_out, 1),
-          (err_word, 1))
+    if not (old_of_new.dtype is kv_len_in.dtype is kv_len_out.dtype is free_pages.dtype is n_free_in.dtype is n_free_out.dtype is
+            err_word.dtype is _I32 and
+            old_of_new.get_device() == kv_len_in.get_device() == kv_len_out.get_device() == free_pages.get_device() ==
+            n_free_in.get_device() == n_free_out.get_device() == dev and
+            old_of_new.is_contiguous() and kv_len_in.is_contiguous() and kv_len_out.is_contiguous() and
+            free_pages.is_contiguous() and old_of_new.numel() >= n_new and kv_len_out.numel() >= n and
+            free_pages.numel() >= num_pages and n_free_in.numel() >= 1 and n_free_out.numel() >= 1 and err_word.numel() >= 1):
+        raise PrismError(-1, what + _INTS)
     s_in, s_out = _table(what, dev, table_in, n), _table(what, dev, table_out, n)
     if table_out.shape[1] != table_in.shape[1]:
         raise PrismError(-1, what + ": tables of one width")
