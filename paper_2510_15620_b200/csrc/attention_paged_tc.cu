@@ -30,7 +30,8 @@
 // heads): two threads per row that meet once a block 625 / 1066 / 288; one thread per row, P V in halves 618 / 1093 / 279; MMAs
 // issued by an elected thread instead of lane 0 (38 instead of 60 issue cycles an instruction) 611 / 1074 / 255; the issuing warp
 // in step 608 / 1070 / 254; exponentials shared with the FMA pipe 570 / 1040 / 254; output rows of 128 bytes 562 / 1017 / 247; one
-// copy of the softmax step, re-entered when a reference moves, and of the issuing step 566 / 1020 / 228.
+// copy of the softmax step, re-entered when a reference moves, and of the issuing step 566 / 1020 / 228; output as TMA boxes
+// 570 / 1027 / 223.
 // Tried and not kept: two threads per row, one deciding the reference for both 650 / 1120 / 286; whole rows in 208 registers
 // (register reallocation) 638 / 1107 / 261; scores double-buffered in blocks of 64 keys 614 / 1103 / 250, again with one copy of
 // the code 709 / 1179 / 279; suspended instead of polled waits 675 / 1151 / 264; the output step unrolled 561 / 1000 / 268.
@@ -138,6 +139,11 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
       : "memory");
 }
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(c0),
+               "r"(c1), "r"(c2)
+               : "memory");
+}
 // Ask the work distributor for a CTA of this grid that has not started; the 16-byte answer lands at `dst`.
 __device__ __forceinline__ void request_unit(uint32_t dst, uint32_t bar) {
   asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(dst), "r"(bar)
@@ -195,8 +201,8 @@ struct UnitReader {
 template <int DH>
 __global__ void __launch_bounds__(kThreads, 1)
 k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-              const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PagedAttnArgs a, int shift, int tpt,
-              float scale_log2) {
+              const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o,
+              const __grid_constant__ PagedAttnArgs a, int shift, int tpt, int boxes_out, float scale_log2) {
   pdl_sync();
   extern __shared__ unsigned char smem_raw[];
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -611,17 +617,22 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       tc_fence_after();
       if (warp_live) {
         if (part < 0) {
-          // This row's O_x / l as bf16, 64 columns at a time through the warp's staging rows (128 bytes each, 16-byte pieces
-          // XOR-swizzled), so that global stores are 128 contiguous bytes per row.
+          // O_x / l as bf16, 64 columns at a time, through the warp's staging rows (128 bytes each, 16-byte pieces XOR-swizzled as
+          // TMA has them).  Where the warp's 32 rows are whole tokens and all live they leave as one box, which the warp need
+          // not wait for (1100 instead of 3500 cycles a unit); else row by row in 128 contiguous bytes.
           const float inv = sees ? 1.f / l : 0.f;
+          const bool whole = boxes_out && __all_sync(0xffffffffu, live);
+          const int tok0 = row0 + x * tpt;
           const int mine = live ? tt * 128 + head : -1;  // head < group <= 128
-          __nv_bfloat16* const ocol = static_cast<__nv_bfloat16*>(a.out) + (long long)(row0 + x * tpt) * a.out_stride +
+          __nv_bfloat16* const ocol = static_cast<__nv_bfloat16*>(a.out) + (long long)tok0 * a.out_stride +
                                       (long long)h * group * DH + (lane & 7) * 8;
 #pragma unroll 1
           for (int pt = 0; pt < DH / 64; ++pt) {
             uint32_t o[64];
             tmem_ld32(t_o + pt * 64, o);
             tmem_ld32(t_o + pt * 64 + 32, o + 32);
+            if (lane == 0) bulk_wait_read<0>();  // the box before this one has been read
+            __syncwarp();
             tmem_ld_wait32(o);
             tmem_ld_wait32(o + 32);
 #pragma unroll
@@ -634,18 +645,27 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
               asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(w4[0]), "r"(w4[1]), "r"(w4[2]), "r"(w4[3])
                            : "memory");
             }
-            __syncwarp();
-#pragma unroll 2
-            for (int i = 0; i < 8; ++i) {
-              const int rr = i * 4 + (lane >> 3);
-              uint4 val;
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                           : "=r"(val.x), "=r"(val.y), "=r"(val.z), "=r"(val.w)
-                           : "r"(stg + rr * 128 + (((lane & 7) ^ (rr & 7)) << 4)));
-              const int to = __shfl_sync(0xffffffffu, mine, rr);
-              if (to >= 0) *reinterpret_cast<uint4*>(ocol + (to >> 7) * a.out_stride + (to & 127) * DH + pt * 64) = val;
+            if (whole) {
+              fence_async_smem();
+              __syncwarp();
+              if (lane == 0) {
+                tma_store_3d(&map_o, stg, pt * 64, h * group, tok0 + quarter * 32 / group);
+                bulk_commit();
+              }
+            } else {
+              __syncwarp();
+#pragma unroll 1
+              for (int i = 0; i < 8; ++i) {
+                const int rr = i * 4 + (lane >> 3);
+                uint4 val;
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(val.x), "=r"(val.y), "=r"(val.z), "=r"(val.w)
+                             : "r"(stg + rr * 128 + (((lane & 7) ^ (rr & 7)) << 4)));
+                const int to = __shfl_sync(0xffffffffu, mine, rr);
+                if (to >= 0) *reinterpret_cast<uint4*>(ocol + (to >> 7) * a.out_stride + (to & 127) * DH + pt * 64) = val;
+              }
+              __syncwarp();
             }
-            __syncwarp();
           }
         } else {
           // partial result, row fastest: the lanes of a warp write side by side
@@ -672,6 +692,7 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
       if (lane == 0) it.release();
       it.advance();
     }
+    if (lane == 0) bulk_wait<0>();  // the last boxes have left shared memory
   }
 
   tc_fence_before();
@@ -683,13 +704,13 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
 }
 
 template <int DH>
-cudaError_t tiles_launch(const TmaDesc& q, const TmaDesc& k, const TmaDesc& v, const PagedAttnArgs& a, int tpt, int grid, int shift,
-                         cudaStream_t st) {
+cudaError_t tiles_launch(const TmaDesc& q, const TmaDesc& k, const TmaDesc& v, const TmaDesc& o, const PagedAttnArgs& a, int tpt,
+                         int boxes_out, int grid, int shift, cudaStream_t st) {
   static std::atomic<unsigned long long> set;
   if (cudaError_t e = ensure_dynamic_smem(k_paged_tiles<DH>, smem_bytes(DH), set)) return e;
   k_paged_tiles<DH><<<grid, kThreads, smem_bytes(DH), st>>>(
-      reinterpret_cast<const CUtensorMap&>(q), reinterpret_cast<const CUtensorMap&>(k), reinterpret_cast<const CUtensorMap&>(v), a,
-      shift, tpt, 1.4426950408889634f / sqrtf((float)DH));
+      reinterpret_cast<const CUtensorMap&>(q), reinterpret_cast<const CUtensorMap&>(k), reinterpret_cast<const CUtensorMap&>(v),
+      reinterpret_cast<const CUtensorMap&>(o), a, shift, tpt, boxes_out, 1.4426950408889634f / sqrtf((float)DH));
   return cudaGetLastError();
 }
 
@@ -700,19 +721,29 @@ cudaError_t launch_paged_tiles(const PagedAttnArgs& a, const PagedPlanShape& s, 
   while ((1 << shift) < a.c.page_size) ++shift;
   const uint64_t dh = a.c.dh, ps = a.c.page_size;
   const int tpt = s.tokens / 2;
-  TmaDesc mq, mk, mv;
+  TmaDesc mq, mk, mv, mo;
   {
     const uint64_t dims[3] = {dh, (uint64_t)a.hq, (uint64_t)a.total_q};
     const uint64_t strides[2] = {dh * 2, (uint64_t)a.q_stride * 2};
     const uint32_t box[3] = {64, (uint32_t)s.group, (uint32_t)tpt};
     if (cudaError_t e = make_tma_nd_bf16(&mq, a.q, 3, dims, strides, box)) return e;
   }
+  // a warp's 32 output rows as one box, where they are whole tokens
+  const int boxes_out = 32 % s.group == 0;
+  mo = mq;
+  if (boxes_out) {
+    const uint64_t dims[3] = {dh, (uint64_t)a.hq, (uint64_t)a.total_q};
+    const uint64_t strides[2] = {dh * 2, (uint64_t)a.out_stride * 2};
+    const uint32_t box[3] = {64, (uint32_t)s.group, (uint32_t)(32 / s.group)};
+    if (cudaError_t e = make_tma_nd_bf16(&mo, a.out, 3, dims, strides, box)) return e;
+  }
   const uint64_t dims[4] = {dh, ps, (uint64_t)a.c.hkv, (uint64_t)a.c.num_pages};
   const uint64_t strides[3] = {dh * 2, ps * dh * 2, (uint64_t)a.c.page_stride * 2};
   const uint32_t box[4] = {64, (uint32_t)(ps < 128 ? ps : 128), 1, 1};
   if (cudaError_t e = make_tma_nd_bf16(&mk, a.c.k, 4, dims, strides, box)) return e;
   if (cudaError_t e = make_tma_nd_bf16(&mv, a.c.v, 4, dims, strides, box)) return e;
-  return a.c.dh == 128 ? tiles_launch<128>(mq, mk, mv, a, tpt, grid, shift, st) : tiles_launch<64>(mq, mk, mv, a, tpt, grid, shift, st);
+  return a.c.dh == 128 ? tiles_launch<128>(mq, mk, mv, mo, a, tpt, boxes_out, grid, shift, st)
+                       : tiles_launch<64>(mq, mk, mv, mo, a, tpt, boxes_out, grid, shift, st);
 }
 
 }  // namespace prism

@@ -133,7 +133,8 @@ int prism_op_attention_paged(const void* q, int64_t q_stride, const prism_kv_cac
   if (int rc = check_shape(n_seq, total_q, max_q_len, n_q_heads, hkv, dh, cache->dtype, impl, &s)) return rc;
   if (max_pages < 0 || table_stride < max_pages || !pages_ok(max_pages, cache->page_size) || !err_word) return PRISM_ERR_INVALID_ARG;
   const int64_t width = (int64_t)n_q_heads * dh;
-  if (q_stride < width || out_stride < width || (q_stride * b) % 16 || (out_stride * b) % 16 || q_stride > ((int64_t)1 << 38))
+  if (q_stride < width || out_stride < width || (q_stride * b) % 16 || (out_stride * b) % 16 || q_stride > ((int64_t)1 << 38) ||
+      out_stride > ((int64_t)1 << 38))
     return PRISM_ERR_INVALID_ARG;
   const PagedPlanBounds bound = paged_plan_bounds(s, hkv, n_seq, total_q);
   if (!plan || !aligned16(plan) || plan_bytes < paged_plan_bytes(bound)) return PRISM_ERR_INVALID_ARG;
