@@ -240,7 +240,7 @@ PRISM_API int prism_op_qknorm_rope_paged(const void* qkv, int64_t qkv_stride, co
  * prism_op_attention_paged_bytes (host only) gives the sizes of plan and workspace; the workspace is scratch of one call
  * and may be NULL when max_pages * page_size <= 512.
  * impl: PRISM_IMPL_AUTO = tensor cores for bf16 at head_dim 64 and 128 (Hq/Hkv <= 128): warp-level MMA with the cache streamed
- * through shared memory when max_q_len * Hq/Hkv <= 16, else tcgen05; CUDA cores otherwise (Hq/Hkv <= 64).
+ * through shared memory when max_q_len * Hq/Hkv <= 32 and Hq/Hkv <= 16, else tcgen05; CUDA cores otherwise (Hq/Hkv <= 64).
  * PRISM_IMPL_SIMT = CUDA cores.  Results do not depend on other sequences' contents; they may differ in rounding between plans
  * that cut a sequence differently. */
 PRISM_API int prism_op_attention_paged_bytes(int32_t n_seq, int32_t total_q, int32_t max_q_len, int32_t n_q_heads,

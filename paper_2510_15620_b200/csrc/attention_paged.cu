@@ -17,9 +17,9 @@ constexpr int kSearch = 1024;
 // One block.  Tiles of s.tokens tokens; a tile whose keys are more than `piece` is cut into equal pieces so that few long
 // sequences still occupy every SM.  Up to kSearch tiles, 32 warps weigh 32 piece lengths against each other (no cut, the
 // longest tile over 2, 3, ... 32): waves of blocks times a mean piece, plus what the longest piece exceeds it by.  Beyond that
-// the SMs are busy anyway and only tiles far longer than the others are cut.  No piece is shorter than the launch's
-// total (keys x heads) over s.target, hence the bounds of paged_plan_bounds.  Tiles are listed from the last to the first: under causal attention a sequence's last tile has the
-// most keys, and the launch should end on light ones.
+// the SMs are busy anyway and only tiles far longer than the others are cut.  No piece is shorter than the launch's total
+// (keys x heads) over s.target, hence the bounds of paged_plan_bounds.  Tiles are listed from the last to the first: under
+// causal attention a sequence's last tile has the most keys, and the launch should end on light ones.
 struct Sums {
   long long a, b, c;
 };
@@ -514,12 +514,14 @@ bool paged_plan_shape(int n_seq, int total_q, int max_q, int hq, int hkv, int dh
   // Tables no wider than min_cut also save the join's launch.
   const bool busy = (long long)n_seq * hkv >= 148;
   s->min_cut = busy ? 2048 : 512;
-  const bool few = (long long)max_q * g <= 16;
+  const bool few = (long long)max_q * g <= 32 && g <= 16;
   if (dtype == 1 && impl == 0 && (dh == 64 || dh == 128) && g <= 128) {
     if (few) {
-      // the whole sequence's new rows fit one 16-row tile; two blocks per SM, together at the memory's rate (6.4 TB/s)
+      // Up to two 16-row tiles a sequence: both read the same keys, the second from L2, and two blocks an SM keep more loads in
+      // flight than the chunk kernel's one (32 rows over 8 k cached tokens, 100 sequences: 568 us against 638; 64 rows: 1100
+      // against 716).  Two blocks per SM, together at the memory's rate (6.4 TB/s); one alone takes 48 GB/s (its ring over the latency)
       s->kind = kPagedTokens, s->rows = 16, s->tokens = 16 / g, s->min_piece = 256, s->slots = 148 * 2;
-      s->ns_key = 4.f * dh / 100.f, s->ns_key_block = 4.f * dh / 6400.f, s->ns_item = 1500.f, s->ns_part = 200.f, s->ns_join = 2500.f;
+      s->ns_key = 3.f + 0.06f * dh, s->ns_key_block = 4.f * dh / 6400.f, s->ns_item = 2500.f, s->ns_part = 200.f, s->ns_join = 2500.f;
     } else {
       // bound by each SM's own tensor core and softmax; a partial result is 133 KB written and read
       s->kind = kPagedTiles, s->rows = 256, s->tokens = 2 * (128 / g), s->min_piece = 1024, s->slots = 148;

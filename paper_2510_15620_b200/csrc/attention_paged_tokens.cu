@@ -1,5 +1,5 @@
-// Attention over a paged cache for few new tokens: at most 16 query rows (token, head of the group) per sequence and
-// key/value head, bf16, head_dim 64 or 128.
+// Attention over a paged cache for few new tokens: at most 32 query rows (token, head of the group) per sequence and
+// key/value head, 16 of them in an item, bf16, head_dim 64 or 128.
 //
 // Bound by reading the cache: every key and value is used for at most 16 rows, 2 * 16 flops a byte at best.  So the
 // kernel is built around the loads.  A work unit is (item of the work list, key/value head); a producer warp keeps a ring

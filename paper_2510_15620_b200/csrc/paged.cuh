@@ -20,7 +20,7 @@ struct PagedCache {
 // Attention over pages: which kernel serves a call.  The choice depends on host-known sizes only and is made by
 // the same function for the work list and for the launch.
 enum PagedKind : int {
-  kPagedTokens = 0,  // few query rows per sequence and key/value head: warp-level MMA, bound by reading the cache
+  kPagedTokens = 0,  // up to 32 query rows per sequence and key/value head: warp-level MMA, bound by reading the cache
   kPagedTiles = 1,   // tcgen05, two 128-row tiles per item
   kPagedSimt = 2,    // CUDA cores: fp32, and head sizes without a tensor-core kernel
 };

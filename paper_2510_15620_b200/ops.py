@@ -3,6 +3,7 @@ device tensors out; work is enqueued on torch's current stream)."""
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
@@ -41,7 +42,7 @@ def _L():
         L.prism_op_embed_encoder.argtypes = [vp, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp]
         L.prism_op_probe_encoder.argtypes = [vp, vp, i32, i32, vp, vp, f32, vp, i32, vp, vp, vp, vp, vp]
         L.prism_op_dequant_w4.argtypes = [vp, i32, i32, i32, vp, vp]
-        i64, pkv = C.c_int64, C.POINTER(_KvCache)
+        i64, pkv = C.c_int64, vp  # pkv: a _KvCache by reference, or its packed bytes
         L.prism_op_page_append.argtypes = [vp, vp, vp, i32, i32, i32, i32, i64, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
         L.prism_op_page_release.argtypes = [vp, i32, vp, vp, i32, i32, i32, i32, i32, i64, vp, i64, vp, vp, vp, vp, vp, vp]
         L.prism_op_qknorm_rope_paged.argtypes = [vp, i64, vp, vp, i32, i32, i32, vp, vp, f32, f32, vp, i64, pkv, vp, vp]
@@ -186,22 +187,21 @@ def _ints(what, dev, *pairs):
             raise PrismError(-1, what + _INTS)
 
 
-def _row_stride(t):
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
-
-
-def _matrix(what, dev, t, dtype, width, rows=0):
-    if (t.dim() != 2 or t.dtype is not _ELEMENT.get(dtype) or t.get_device() != dev or t.shape[1] != width or t.shape[0] < rows or
-            (t.stride(1) != 1 and t.numel() > 1)):
+def _matrix(what, dev, t, element, width, rows=0):
+    shape, stride = t.shape, t.stride()
+    if (len(shape) != 2 or t.dtype is not element or t.get_device() != dev or shape[1] != width or shape[0] < rows or
+            (stride[1] != 1 and t.numel() > 1)):
         raise PrismError(-1, what + ": a matrix of the stated element type, width and rows, without gaps inside a row")
-    return _row_stride(t)
+    return stride[0] if shape[0] > 1 else max(width, stride[0])
 
 
 def _table(what, dev, t, n):
-    if (t.dim() != 2 or t.dtype is not _I32 or t.get_device() != dev or t.shape[0] < n or
-            (t.stride(1) != 1 and t.shape[1] > 1 and t.numel() > 0)):
+    """Width and row stride."""
+    shape, stride = t.shape, t.stride()
+    if (len(shape) != 2 or t.dtype is not _I32 or t.get_device() != dev or shape[0] < n or
+            (stride[1] != 1 and shape[1] > 1 and t.numel() > 0)):
         raise PrismError(-1, what + ": an int32 block table with a row per sequence")
-    return _row_stride(t)
+    return shape[1], stride[0] if shape[0] > 1 else max(shape[1], stride[0])
 
 
 def _bytes(what, dev, t):
@@ -210,15 +210,20 @@ def _bytes(what, dev, t):
     return t.numel() * t.element_size()
 
 
-def _cache(what, dev, k, v, dtype):
-    if (k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype is not _ELEMENT.get(dtype) or
-            v.dtype is not k.dtype or k.get_device() != dev or v.get_device() != dev):
+_pack_cache = struct.Struct("@PPqiiiii").pack  # the fields of _KvCache; four times as fast as filling one
+
+
+def _cache(what, dev, k, v, element, dtype):
+    """Heads, head_dim and the packed prism_kv_cache."""
+    shape, stride = k.shape, k.stride()
+    if (len(shape) != 4 or shape != v.shape or stride != v.stride() or k.dtype is not element or v.dtype is not element or
+            k.get_device() != dev or v.get_device() != dev):
         raise PrismError(-1, what + ": k and v caches of one layout and the stated element type")
-    pages, heads, page, dh = k.shape
-    s0, s1, s2, s3 = k.stride()
+    pages, heads, page, dh = shape
+    s0, s1, s2, s3 = stride
     if s3 != 1 or s2 != dh or (s1 != page * dh and heads > 1):
         raise PrismError(-1, what + ": a page of the cache has gaps inside")
-    return _KvCache(k.data_ptr(), v.data_ptr(), s0 if pages > 1 else heads * page * dh, pages, page, heads, dh, dtype)
+    return heads, dh, _pack_cache(k.data_ptr(), v.data_ptr(), s0 if pages > 1 else heads * page * dh, pages, page, heads, dh, dtype)
 
 
 def prism_op_page_append(len_new, kv_len_in, kv_len_out, page_size, num_pages, block_table, free_pages, n_free_in, n_free_out,
@@ -236,9 +241,9 @@ def prism_op_page_append(len_new, kv_len_in, kv_len_out, page_size, num_pages, b
             kv_len_in.numel() >= n and kv_len_out.numel() >= n and free_pages.numel() >= num_pages and n_free_in.numel() >= 1 and
             n_free_out.numel() >= 1 and cu_q.numel() > n and pos.numel() >= total and err_word.numel() >= 1):
         raise PrismError(-1, what + _INTS)
-    stride = _table(what, dev, block_table, n)
+    width, stride = _table(what, dev, block_table, n)
     rc = _L().prism_op_page_append(len_new.data_ptr(), kv_len_in.data_ptr(), kv_len_out.data_ptr(), n, page_size, num_pages,
-                                   block_table.shape[1], stride, block_table.data_ptr(), free_pages.data_ptr(),
+                                   width, stride, block_table.data_ptr(), free_pages.data_ptr(),
                                    n_free_in.data_ptr(), n_free_out.data_ptr(), total, cu_q.data_ptr(), pos.data_ptr(),
                                    slot_map.data_ptr(), err_word.data_ptr(), _stream_of(dev))
     if rc:
@@ -258,11 +263,11 @@ def prism_op_page_release(old_of_new, kv_len_in, kv_len_out, page_size, num_page
             free_pages.is_contiguous() and old_of_new.numel() >= n_new and kv_len_out.numel() >= n and
             free_pages.numel() >= num_pages and n_free_in.numel() >= 1 and n_free_out.numel() >= 1 and err_word.numel() >= 1):
         raise PrismError(-1, what + _INTS)
-    s_in, s_out = _table(what, dev, table_in, n), _table(what, dev, table_out, n)
-    if table_out.shape[1] != table_in.shape[1]:
+    (width, s_in), (w_out, s_out) = _table(what, dev, table_in, n), _table(what, dev, table_out, n)
+    if w_out != width:
         raise PrismError(-1, what + ": tables of one width")
     rc = _L().prism_op_page_release(old_of_new.data_ptr(), n_new, kv_len_in.data_ptr(), kv_len_out.data_ptr(), n, page_size,
-                                    num_pages, shared_pages, table_in.shape[1], s_in, table_in.data_ptr(), s_out,
+                                    num_pages, shared_pages, width, s_in, table_in.data_ptr(), s_out,
                                     table_out.data_ptr(), free_pages.data_ptr(), n_free_in.data_ptr(), n_free_out.data_ptr(),
                                     err_word.data_ptr(), _stream_of(dev))
     if rc:
@@ -272,18 +277,21 @@ def prism_op_page_release(old_of_new, kv_len_in, kv_len_out, page_size, num_page
 def prism_op_qknorm_rope_paged(qkv, dtype, pos, slot_map, n_q_heads, qk_norm, g_q, g_k, eps, theta, q_out, k_cache, v_cache,
                                err_word):
     what = "qknorm_rope_paged"
-    dev = _device(what, err_word)
-    c = _cache(what, dev, k_cache, v_cache, dtype)
+    dev, element = _device(what, err_word), _ELEMENT.get(dtype)
+    heads, dh, cache = _cache(what, dev, k_cache, v_cache, element, dtype)
     rows = qkv.shape[0]
-    s_in = _matrix(what, dev, qkv, dtype, (n_q_heads + 2 * c.n_kv_heads) * c.head_dim)
-    s_out = _matrix(what, dev, q_out, dtype, n_q_heads * c.head_dim, rows)
-    _ints(what, dev, (pos, rows), (slot_map, rows), (err_word, 1))
-    if qk_norm:
-        for g in (g_q, g_k):
-            if g.dtype is not qkv.dtype or g.get_device() != dev or not g.is_contiguous() or g.numel() != c.head_dim:
-                raise PrismError(-1, what + ": gains of head_dim elements of the stated type")
+    s_in = _matrix(what, dev, qkv, element, (n_q_heads + 2 * heads) * dh)
+    s_out = _matrix(what, dev, q_out, element, n_q_heads * dh, rows)
+    if not (pos.dtype is slot_map.dtype is err_word.dtype is _I32 and pos.get_device() == slot_map.get_device() == dev and
+            pos.is_contiguous() and slot_map.is_contiguous() and pos.numel() >= rows and slot_map.numel() >= rows and
+            err_word.numel() >= 1):
+        raise PrismError(-1, what + _INTS)
+    if qk_norm and not (g_q is not None and g_k is not None and g_q.dtype is g_k.dtype is element and
+                        g_q.get_device() == g_k.get_device() == dev and g_q.is_contiguous() and g_k.is_contiguous() and
+                        g_q.numel() == g_k.numel() == dh):
+        raise PrismError(-1, what + ": gains of head_dim elements of the stated type")
     rc = _L().prism_op_qknorm_rope_paged(qkv.data_ptr(), s_in, pos.data_ptr(), slot_map.data_ptr(), rows, n_q_heads, qk_norm,
-                                         _p(g_q), _p(g_k), eps, theta, q_out.data_ptr(), s_out, c, err_word.data_ptr(),
+                                         _p(g_q), _p(g_k), eps, theta, q_out.data_ptr(), s_out, cache, err_word.data_ptr(),
                                          _stream_of(dev))
     if rc:
         raise PrismError(rc, what)
@@ -312,13 +320,14 @@ def prism_op_attention_paged_plan(cu_q, kv_len, total_q, max_q_len, n_q_heads, n
 def prism_op_attention_paged(q, k_cache, v_cache, block_table, plan, n_seq, max_q_len, n_q_heads, dtype, out, workspace, err_word,
                              impl=PRISM_IMPL_AUTO):
     what = "attention_paged"
-    dev = _device(what, err_word)
-    c = _cache(what, dev, k_cache, v_cache, dtype)
-    rows, width = q.shape[0], n_q_heads * c.head_dim
-    s_q, s_out = _matrix(what, dev, q, dtype, width), _matrix(what, dev, out, dtype, width, rows)
-    _ints(what, dev, (err_word, 1))
-    stride = _table(what, dev, block_table, n_seq)
-    rc = _L().prism_op_attention_paged(q.data_ptr(), s_q, c, block_table.data_ptr(), stride, block_table.shape[1], plan.data_ptr(),
+    dev, element = _device(what, err_word), _ELEMENT.get(dtype)
+    heads, dh, cache = _cache(what, dev, k_cache, v_cache, element, dtype)
+    rows, width = q.shape[0], n_q_heads * dh
+    s_q, s_out = _matrix(what, dev, q, element, width), _matrix(what, dev, out, element, width, rows)
+    if err_word.dtype is not _I32 or err_word.numel() < 1:
+        raise PrismError(-1, what + _INTS)
+    max_pages, stride = _table(what, dev, block_table, n_seq)
+    rc = _L().prism_op_attention_paged(q.data_ptr(), s_q, cache, block_table.data_ptr(), stride, max_pages, plan.data_ptr(),
                                        _bytes(what, dev, plan), n_seq, rows, max_q_len, n_q_heads, impl, out.data_ptr(), s_out,
                                        _p(workspace), 0 if workspace is None else _bytes(what, dev, workspace),
                                        err_word.data_ptr(), _stream_of(dev))

@@ -365,13 +365,16 @@ class Call:
         return self.check()
 
 
-TOKENS = [  # one to a few new tokens, at most 16 (token, head) rows: lengths around page, stage and piece borders
+TOKENS = [  # one to a few new tokens, at most 32 (token, head) rows: lengths around page, stage and piece borders
     (16, 8, 128, 16, [1] * 9, [1, 2, 15, 16, 17, 63, 64, 65, 300]),
     (32, 8, 128, 64, [1, 4, 2, 0, 3], [70, 4, 1, 50, 999]),                 # q_len 2 of 1 key: a row that sees nothing
     (16, 16, 64, 16, [1, 1, 16, 7], [0, 33, 20, 129]),                      # no keys at all
     (8, 1, 64, 32, [1, 2, 1], [31, 2100, 5000]),                            # cut into pieces
     (16, 1, 128, 128, [1, 1], [127, 3001]),
     (12, 4, 128, 256, [5, 1], [256, 777]),
+    (16, 8, 128, 16, [16, 3, 9, 0, 1], [16, 200, 2500, 5, 1]),              # two items of 16 rows a sequence
+    (28, 4, 64, 32, [4, 1, 3], [4, 1500, 40]),                              # two tokens of seven heads an item
+    (16, 1, 128, 128, [2, 1], [2, 3001]),                                   # one token an item
 ]
 TILES = [  # chunks
     (16, 8, 128, 16, [17, 64, 65, 1, 128, 129], [17, 100, 65, 40, 500, 129]),
@@ -688,3 +691,42 @@ def test_a_request_over_the_cache(P, dtype):
     for _ in range(3):
         step(kv[:4], table2[:4], [1] * 4, keep.tolist())
     step(kv[:4], table2[:4], [20, 1, 7, 33], keep.tolist())
+
+
+# ------------------------------------------------------------------------------------------------ the Python layer's refusals
+def test_tensors_that_the_kernels_would_misread_are_refused(P):
+    c = Call(P, np.random.default_rng(50), [1, 2], [40, 90], 16, 8, 128, BF16, 1, 16).run()
+    h = lambda t: t.half() if t.dtype == torch.bfloat16 else t
+
+    def refused(fn, *args):
+        with pytest.raises(P.PrismError) as e:
+            fn(*args)
+        assert e.value.status == -1
+
+    attend = lambda q=c.qd, k=c.kd, v=c.vd, table=c.tabled, out=c.out, ws=c.ws, err=c.err: P.ops.prism_op_attention_paged(
+        q, k, v, table, c.plan, c.n, c.max_q, c.hq, BF16, out, ws, err)
+    refused(attend, h(c.qd))                                             # another element type
+    refused(attend, c.qd[:, :-16])                                       # another width
+    refused(attend, c.qd, h(c.kd), h(c.vd))
+    refused(attend, c.qd, c.kd.contiguous(), c.vd)                       # two layouts
+    refused(attend, c.qd, c.kd.transpose(1, 2), c.vd.transpose(1, 2))    # gaps inside a page
+    refused(attend, c.qd, c.kd, c.vd, c.tabled.long())
+    refused(attend, c.qd, c.kd, c.vd, c.tabled[:1])                      # fewer rows than sequences
+    refused(attend, c.qd, c.kd, c.vd, c.tabled, c.out[:2])
+    refused(attend, c.qd, c.kd, c.vd, c.tabled, c.out, c.ws[:64].cpu())
+    refused(attend, c.qd.cpu())
+    refused(attend, c.qd, c.kd, c.vd, c.tabled, c.out, c.ws, c.err.long())
+    i = i32(np.arange(8))
+    rope = lambda qkv, g, q=c.out[:, :64]: P.ops.prism_op_qknorm_rope_paged(qkv, FP32, i, i, 1, 1, g, g, 1e-6, 1e4, q, c.kd, c.vd, c.err)
+    x = torch.zeros(4, 3 * 64, device="cuda")
+    cache = torch.zeros(2, 1, 1, 16, 64, device="cuda")
+    one = lambda g, pos=i: P.ops.prism_op_qknorm_rope_paged(x, FP32, pos, i, 1, 1, g, g, 1e-6, 1e4, torch.zeros(4, 64, device="cuda"),
+                                                            cache[0], cache[1], c.err)
+    refused(rope, x, torch.ones(64, device="cuda"))                      # a bf16 cache for fp32 rows
+    refused(one, None)
+    refused(one, torch.ones(32, device="cuda"))
+    refused(one, torch.ones(64, device="cuda"), i[:2])                   # fewer positions than rows
+    one(torch.ones(64, device="cuda"))
+    refused(P.ops.prism_op_page_append, i, i, i, 16, 8, i.view(8, 1), i, i, i, i, i, i, c.err)   # cu_q one entry short
+    refused(P.ops.prism_op_page_append, i[::2], i, i, 16, 8, i.view(8, 1), i, i, i, i, i, i, c.err)
+    torch.cuda.synchronize()
