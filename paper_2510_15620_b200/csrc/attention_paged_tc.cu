@@ -87,13 +87,12 @@ __device__ __forceinline__ void tmem_ld_wait32(uint32_t* r) {
 }
 // 2^(s * scale - ms) of 32 scores as 16 packed bf16 pairs (key 2 e in the low half), and their sum.
 // The special-function unit gives an SM 16 exponentials a clock, i.e. a 128 x 128 block of scores takes as long as its two
-// products; kOnFma of the 16 pairs are therefore formed on the FMA pipe: x = n + f, n = round(x) (adding 1.5 * 2^23 leaves n in
+// products; three of the 16 pairs are therefore formed on the FMA pipe: x = n + f, n = round(x) (adding 1.5 * 2^23 leaves n in
 // the low bits), 2^f by the degree-5 minimax polynomial on [-1/2, 1/2] (relative error 2^-23.6, as good as ex2.approx), n added
 // to the exponent field.  x is clamped to [-125, 126]: a masked score comes out as 2^-125 instead of 0 beside a sum of at least
 // 1, and one beyond fp32 range is still seen by the range check.
 // Measured (2368 tokens behind 16 k / 1024 behind 64 k, 32 query heads): none 607 / 1070 us, 2 pairs 572 / 1041, 3 568 / 1039,
 // 4 575 / 1043; short sequences indifferent.
-constexpr int kOnFma = 3;
 __device__ __forceinline__ void exp_chunk(const uint32_t* s, uint64_t sc2, float ms, uint32_t* pk, float& sum) {
   const uint64_t nm2 = f2_pack(-ms, -ms);
   const float kMagic = 12582912.f;
@@ -103,7 +102,7 @@ __device__ __forceinline__ void exp_chunk(const uint32_t* s, uint64_t sc2, float
     const uint64_t xv = f2_fma(f2_pack(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), sc2, nm2);
     float x0, x1, p0, p1;
     f2_unpack(xv, x0, x1);
-    if ((e * kOnFma) / 16 != ((e + 1) * kOnFma) / 16) {
+    if (e % 5 == 2) {
       const uint64_t xc = f2_pack(fminf(fmaxf(x0, -125.f), 126.f), fminf(fmaxf(x1, -125.f), 126.f));
       const uint64_t t = f2_add(xc, f2_pack(kMagic, kMagic));
       const uint64_t f = f2_fma(f2_add(t, f2_pack(-kMagic, -kMagic)), f2_pack(-1.f, -1.f), xc);
