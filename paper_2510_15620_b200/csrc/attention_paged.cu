@@ -70,13 +70,13 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restri
   for (int i = i0; i < i1; ++i) {
     const int a = cu[i], b = cu[i + 1];
     if (a < 0 || b < a || b > total_q || b - a > max_q || kv_len[i] < 0) bad = true;
-    else mine.a += (b - a + sh.tokens - 1) / sh.tokens;
+    else mine.a += ((unsigned)(b - a) + sh.tokens - 1) / sh.tokens;
   }
   Sums at = plan_scan(mine, warp_tot, tot);
   bad = __syncthreads_or(bad);
   for (int i = i0; !bad && i < i1; ++i) {
     s_tile[i] = (int)at.a;
-    at.a += (cu[i + 1] - cu[i] + sh.tokens - 1) / sh.tokens;
+    at.a += ((unsigned)(cu[i + 1] - cu[i]) + sh.tokens - 1) / sh.tokens;
   }
   const int n_tiles = bad ? 0 : (int)tot.a;
   if (tid == 0) s_tile[n] = n_tiles;
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restri
   if (n_tiles <= kSearch) {
     longest = __reduce_max_sync(0xffffffffu, s_longest[tid & 31]);
     const int j = tid >> 5, lane = tid & 31;
-    unsigned len = j == 0 ? 0x7fffffffu : (unsigned)((longest + j) / (j + 1) + sh.piece_unit - 1) / sh.piece_unit * sh.piece_unit;
+    unsigned len = j == 0 ? 0x7fffffffu : (((unsigned)longest + j) / (j + 1) + sh.piece_unit - 1) / sh.piece_unit * sh.piece_unit;
     if (len < piece) len = (unsigned)min(piece, 0x7fffffffll);
     unsigned items_n = 0, parts_n = 0;
     for (int t = lane; t < n_tiles; t += 32) {
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restri
       const long long cuts = r.keys > sh.min_cut ? (r.keys + piece - 1) / piece : 1;
       if (cuts > 1) {
         len = (int)(((r.keys + cuts - 1) / cuts + sh.piece_unit - 1) / sh.piece_unit * sh.piece_unit);
-        c.a = (r.keys + len - 1) / len;
+        c.a = ((long long)r.keys + len - 1) / len;  // (a length may be as large as an int holds)
       } else {
         c.a = 1;
       }

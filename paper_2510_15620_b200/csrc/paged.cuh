@@ -60,7 +60,7 @@ __device__ __forceinline__ void paged_item_check(PagedItem& it, int max_pages, i
   const long long cap = (long long)max_pages << shift;
   if (it.k1 > cap) {
     if (threadIdx.x == 0) atomicOr(err, kErrBadPage);
-    it.k1 = (int)cap;
+    it.k1 = (int)cap, it.k0 = min(it.k0, it.k1);  // (what counts keys from k0 on stays below 2^31)
   }
   if (it.part >= 0 && !ws) it.k1 = it.k0 = 0, it.part = -1;
 }

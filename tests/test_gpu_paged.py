@@ -562,6 +562,27 @@ def test_attention_with_a_plan_for_longer_tables_and_no_workspace(P):
         assert int(c.err.item()) == 16
 
 
+@pytest.mark.parametrize("n,new,hq,hkv,dtype", [(4, 1, 16, 8, BF16), (4, 40, 16, 8, BF16), (4, 40, 16, 8, FP32), (1, 1, 8, 1, BF16),
+                                                (40, 200, 8, 1, BF16), (1100, 1, 8, 1, BF16)])
+def test_plan_for_the_longest_lengths_an_int_holds(P, n, new, hq, hkv, dtype):
+    """Lengths of 2^31 - 1 and a little less, behind a block table of 700 tokens: reported, and the plan stays inside its buffer."""
+    rng = np.random.default_rng(34)
+    c = Call(P, rng, [new] * n, [700 if i < 3 else 300 for i in range(n)], hq, hkv, 128, dtype, 1, 16)
+    room = torch.full((c.plan.numel() + 65536,), 255, dtype=torch.uint8, device="cuda")
+    c.plan = room[32768:32768 + c.plan.numel()]
+    for kv in (rng.integers((1 << 31) - 3000, 1 << 31, size=n), np.full(n, (1 << 31) - 1)):
+        c.err.zero_()
+        c.kvd.copy_(i32(kv))
+        c.make_plan()
+        torch.cuda.synchronize()
+        assert int(c.err.item()) == 0
+        assert (room[:32768] == 255).all() and (room[-32768:] == 255).all()
+        c.attend()
+        torch.cuda.synchronize()
+        assert int(c.err.item()) == 16
+        assert (c.outd[:, :16] == 3).all() and (c.outd[:2] == 3).all() and (c.outd[-3:] == 3).all()
+
+
 def test_cache_beyond_32_bit_offsets(P):
     """Pages 2^24 elements apart: the last ones start past 2^31 elements."""
     stride, pages, hkv, dh, page = 1 << 24, 200, 2, 128, 16
