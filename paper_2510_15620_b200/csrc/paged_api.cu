@@ -12,9 +12,9 @@ int st_of(cudaError_t e) {
 cudaStream_t S(void* s) { return reinterpret_cast<cudaStream_t>(s); }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool page_size_ok(int32_t p) { return p >= 16 && p <= 256 && (p & (p - 1)) == 0; }
-// slots, and the tokens a block-table row can name, are counted in 32 bits
+// slots, and the tokens a block-table row can name, are counted in 32 bits, and so is the end of the last tile of keys (128)
 bool pages_ok(int32_t num_pages, int32_t page_size) {
-  return num_pages >= 0 && page_size_ok(page_size) && ((int64_t)num_pages + 1) * page_size <= INT32_MAX;
+  return num_pages >= 0 && page_size_ok(page_size) && (int64_t)num_pages * page_size <= ((int64_t)1 << 31) - 512;
 }
 int32_t elem(int32_t dtype) { return dtype == PRISM_BF16 ? 2 : 4; }
 

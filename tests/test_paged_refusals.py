@@ -154,3 +154,11 @@ def test_host_tensors_are_refused():
     assert e.value.status == INVALID
     with pytest.raises(P.PrismError):
         ops.prism_op_attention_paged_plan(i, i[:4], 8, 2, 4, 2, 64, BF16, 1, i, i)
+
+
+def test_pages_are_limited_so_that_every_tile_of_keys_ends_below_2_31(L, buf):
+    p, most = buf[1], (1 << 27) - 32              # 16 * most = 2^31 - 512
+    for pages, want in ((most, OK), (most + 1, INVALID)):
+        assert attn(L, p, n=0, max_pages=pages, stride=pages) == want
+        assert attn(L, p, n=0, c=cache(p, num_pages=pages)) == want
+        assert rope(L, p, rows=0, c=cache(p, num_pages=pages)) == want
