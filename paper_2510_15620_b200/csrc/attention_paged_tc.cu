@@ -17,8 +17,7 @@
 //               the order PV_A(g) S_A(g+1) PV_B(g) S_B(g+1), each P V in two halves of 64 keys
 //   warps 2..5  softmax of A, warps 6..9 of B: one thread per row (no exchange between threads: the row's reference and sum
 //               are its own), exponentials against a reference that starts as the row's score on the piece's first key (a row
-//               that sees any key of a piece sees that one) and moves, by whole powers of two, only when a sum threatens
-//               fp32 range
+//               that sees any key of a piece sees that one) and moves only when a sum threatens fp32 range
 // Tensor memory: S_A, S_B, O_A, O_B.  P_x(g) overlies S_x(g).  Rows that no token owns are not computed; a warp without any
 // live row only keeps the barriers' phases.
 //
@@ -85,12 +84,17 @@ __device__ __forceinline__ void tmem_ld_wait32(uint32_t* r) {
                :
                : "memory");
 }
+__device__ __forceinline__ float clamp_exponent(float x) {  // to [-127, 126]; a NaN stays one
+  float y;
+  asm("max.NaN.f32 %0, %1, 0fC2FE0000;\n\tmin.NaN.f32 %0, %0, 0f42FC0000;" : "=f"(y) : "f"(x));
+  return y;
+}
 // 2^(s * scale - ms) of 32 scores as 16 packed bf16 pairs (key 2 e in the low half), and their sum.
 // The special-function unit gives an SM 16 exponentials a clock, i.e. a 128 x 128 block of scores takes as long as its two
 // products; three of the 16 pairs are therefore formed on the FMA pipe: x = n + f, n = round(x) (adding 1.5 * 2^23 leaves n in
-// the low bits), 2^f by the degree-5 minimax polynomial on [-1/2, 1/2] (relative error 2^-23.6, as good as ex2.approx), n added
-// to the exponent field.  x is clamped to [-125, 126]: a masked score comes out as 2^-125 instead of 0 beside a sum of at least
-// 1, and one beyond fp32 range is still seen by the range check.
+// the low bits), 2^f by the degree-5 minimax polynomial on [-1/2, 1/2] (relative error 2^-23.6, as good as ex2.approx), times
+// 2^n put together in the exponent field.  x is clamped to [-127, 126]: at -127 the field is 0, so a masked score gives exactly
+// 0, and one beyond fp32 range is still seen by the range check.  A NaN passes the clamp and the product.
 // Measured (2368 tokens behind 16 k / 1024 behind 64 k, 32 query heads): none 607 / 1070 us, 2 pairs 572 / 1041, 3 568 / 1039,
 // 4 575 / 1043; short sequences indifferent.
 __device__ __forceinline__ void exp_chunk(const uint32_t* s, uint64_t sc2, float ms, uint32_t* pk, float& sum) {
@@ -103,7 +107,7 @@ __device__ __forceinline__ void exp_chunk(const uint32_t* s, uint64_t sc2, float
     float x0, x1, p0, p1;
     f2_unpack(xv, x0, x1);
     if (e % 5 == 2) {
-      const uint64_t xc = f2_pack(fminf(fmaxf(x0, -125.f), 126.f), fminf(fmaxf(x1, -125.f), 126.f));
+      const uint64_t xc = f2_pack(clamp_exponent(x0), clamp_exponent(x1));
       const uint64_t t = f2_add(xc, f2_pack(kMagic, kMagic));
       const uint64_t f = f2_fma(f2_add(t, f2_pack(-kMagic, -kMagic)), f2_pack(-1.f, -1.f), xc);
       uint64_t p = f2_fma(f2_pack(0.0013277939f, 0.0013277939f), f, f2_pack(0.009675758f, 0.009675758f));
@@ -111,11 +115,11 @@ __device__ __forceinline__ void exp_chunk(const uint32_t* s, uint64_t sc2, float
       p = f2_fma(p, f, f2_pack(0.24022114f, 0.24022114f));
       p = f2_fma(p, f, f2_pack(0.69314694f, 0.69314694f));
       p = f2_fma(p, f, f2_pack(1.0000001f, 1.0000001f));
-      float q0, q1, t0, t1;
-      f2_unpack(p, q0, q1);
+      float t0, t1;
       f2_unpack(t, t0, t1);
-      p0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
-      p1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
+      p = f2_mul(p, f2_pack(__uint_as_float((__float_as_uint(t0) << 23) + 0x3f800000u),
+                            __uint_as_float((__float_as_uint(t1) << 23) + 0x3f800000u)));
+      f2_unpack(p, p0, p1);
     } else {
       p0 = ex2(x0), p1 = ex2(x1);
     }
@@ -542,7 +546,8 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
           };
           tmem_ld32(t_s, buf[0]);
           tmem_ld_wait32(buf[0]);
-          if (j == 0) ms = sees ? __uint_as_float(buf[0][0]) * scale_log2 : 0.f;
+          // (kept finite: the first score may be -inf while others are not)
+          if (j == 0) ms = sees ? fmaxf(__uint_as_float(buf[0][0]) * scale_log2, -1e30f) : 0.f;
           bool moved = false;  // this half is being done again, with a new reference
 #pragma unroll 1
           for (int i = 0; i < 2;) {
@@ -553,11 +558,12 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
             if (i == 0) tmem_ld32(t_s + 64, buf[0]);
             sum += chunk(2 * i + 1, buf[1], pk + 16);
             if (!moved && __any_sync(0xffffffffu, live && !(sum <= kBigSum))) {
-              // Rare: rows whose largest exponent is beyond 2^64 move their reference up by d = ceil(that exponent); what was
-              // accumulated under the old one is scaled by 2^-d (exact).  This half's P has not been stored, so its scores
-              // are still there; the other half's product, if it was issued, has to be in O first.
+              // Rare: rows whose largest score is 64 or more above their reference take it as the new one, and what was
+              // accumulated under the old one is scaled.  (Not old + difference: behind a first score of -1e30 that loses the
+              // new one's digits.)  This half's P has not been stored, so its scores are still there; the other half's
+              // product, if it was issued, has to be in O first.
               if (i == 0) tmem_ld_wait32(buf[0]);
-              float xmax = -INFINITY;
+              float smax = -INFINITY;
 #pragma unroll 1
               for (int v = 0; v < 64; v += 4) {
                 uint32_t o[4];
@@ -565,10 +571,9 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  if (kb + i * 64 + v + e < lim) xmax = fmaxf(xmax, fmaf(__uint_as_float(o[e]), scale_log2, -ms));
+                  if (kb + i * 64 + v + e < lim) smax = fmaxf(smax, __uint_as_float(o[e]) * scale_log2);
               }
-              const float d = xmax > 64.f ? ceilf(xmax) : 0.f;
-              const float f = exp2f(-d);
+              const float to = smax - ms > 64.f ? smax : ms, f = exp2f(ms - to);
               if (i == 1) {
                 if (!warp_wait(b_half + 8 * x, gc & 1, err, abort_flag)) { ok = false; break; }
                 tc_fence_after();
@@ -586,7 +591,7 @@ k_paged_tiles(const __grid_constant__ CUtensorMap map_q, const __grid_constant__
                 tmem_st_wait();
               }
               l *= f;
-              ms += d;
+              ms = to;
               tmem_ld32(t_s + i * 64, buf[0]);
               moved = true;
               continue;

@@ -562,6 +562,67 @@ def test_attention_with_a_plan_for_longer_tables_and_no_workspace(P):
         assert int(c.err.item()) == 16
 
 
+# ------------------------------------------------------------------------------------------------ scores that are no numbers
+def check_with_nans(c, size):
+    """As Call.check, for rows whose plain form may be NaN; size: what the rounding of a score is relative to."""
+    torch.cuda.synchronize()
+    assert int(c.err.item()) == 0
+    out, avg, _ = attention(c.q.astype(np.float64), c.k.astype(np.float64), c.v.astype(np.float64), c.table, c.cu, c.kv, c.causal)
+    tol = attention_tolerance(out, avg, size, c.dh, int(c.kv.max()), c.dtype == BF16)
+    got = host(c.out).reshape(out.shape)
+    a, b = int(c.cu[0]), int(c.cu[-1])
+    nan = np.isnan(out)[a:b]
+    assert (np.isnan(got)[a:b] == nan).all()
+    assert (nan | (np.abs(got - out) <= tol)[a:b]).all()
+    return nan
+
+
+def sizes_of(c, k):
+    return attention(c.q.astype(np.float64), k.astype(np.float64), c.v.astype(np.float64), c.table, c.cu, c.kv, c.causal)[2]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("new", [1, 200])
+@pytest.mark.parametrize("low", [-1e9, -1e30, -np.inf])
+def test_attention_over_keys_that_weigh_nothing(P, new, dtype, low):
+    """Every 128th key, the first of every piece among them, has a score so low that its weight is 0: the others' do not
+    depend on it, nor does their rounding."""
+    c = Call(P, np.random.default_rng(31), [new, new], [300, 2600], 16, 8, 128, dtype, 1, 16)
+    c.q[:, :, 0] = 1.0
+    plain = c.k.copy()
+    for s in range(2):
+        for t in range(0, int(c.kv[s]), 128):
+            p, r = c.table[s, t // 16], t % 16
+            c.k[p, :, r, 0] = low if dtype == FP32 else round_to_bf16(np.float32([low]))[0]
+            plain[p, :, r] = 0.0
+    c.kd.copy_(dev(c.k, dtype))
+    c.qd.copy_(dev(c.q.reshape(c.q.shape[0], -1), dtype))
+    c.make_plan()
+    c.attend()
+    assert not check_with_nans(c, sizes_of(c, plain)).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("at", [4, 14, 25, 31])
+def test_attention_over_a_key_that_is_nan(P, at, dtype):
+    """A NaN in a key makes the rows that see it NaN, and no others."""
+    c = Call(P, np.random.default_rng(32), [200, 200, 1], [300, 2600, 200], 16, 8, 128, dtype, 1, 16)
+    for s, t in ((0, 160 + at), (1, 2496 + at), (2, 64 + at)):
+        c.k[c.table[s, t // 16], :, t % 16, 3] = np.nan
+    c.kd.copy_(dev(c.k, dtype))
+    c.make_plan()
+    c.attend()
+    nan = check_with_nans(c, sizes_of(c, c.k))
+    assert nan[160 + at - 100:200].all() and not nan[:160 + at - 100].any() and nan[400].all()
+    c = Call(P, np.random.default_rng(33), [1, 2], [300, 2600], 16, 8, 128, dtype, 1, 16)
+    c.k[c.table[0, 9], :, at % 16, 3] = np.nan
+    c.kd.copy_(dev(c.k, dtype))
+    c.make_plan()
+    c.attend()
+    nan = check_with_nans(c, sizes_of(c, c.k))
+    assert nan[0].all() and not nan[1:].any()
+
+
 @pytest.mark.parametrize("n,new,hq,hkv,dtype", [(4, 1, 16, 8, BF16), (4, 40, 16, 8, BF16), (4, 40, 16, 8, FP32), (1, 1, 8, 1, BF16),
                                                 (40, 200, 8, 1, BF16), (1100, 1, 8, 1, BF16)])
 def test_plan_for_the_longest_lengths_an_int_holds(P, n, new, hq, hkv, dtype):
