@@ -3,12 +3,12 @@
 //
 // Bound by reading the cache: every key and value is used for at most 16 rows, 2 * 16 flops a byte at best.  So the
 // kernel is built around the loads.  A work unit is (item of the work list, key/value head); a producer warp keeps a ring
-// of kStages stages of 64 keys and their values in flight, one TMA box per page (the page table's indirection costs one
-// load per page, taken a stage ahead), and four warps each take 16 of a stage's keys with warp-level MMAs, a running maximum
+// of kStages stages of 64 keys and their values in flight, one TMA box per page (page numbers are read 32 boxes at a
+// time, a batch ahead), and four warps each take 16 of a stage's keys with warp-level MMAs, a running maximum
 // and a running sum of their own.  No warp waits for another until the end, where the four results meet in shared memory.
 // The warp-level MMA is chosen on purpose: sixteen rows would leave seven eighths of a 128-row tcgen05 tile empty and put
 // its tensor-memory round trips on the path of a kernel that only has to keep up with memory.
-// Rounding: probabilities become bf16 for the second product (relative 2^-9, as in the packed attention kernels); the sum
+// Rounding: probabilities become bf16 for the second product (relative 2^-8, as in the packed attention kernels); the sum
 // they are divided by is taken in fp32 before that.
 #include <math.h>
 
