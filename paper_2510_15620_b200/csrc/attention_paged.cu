@@ -510,8 +510,9 @@ bool paged_plan_shape(int n_seq, int total_q, int max_q, int hq, int hkv, int dh
   s->group = g;
   s->piece_unit = 128;
   s->target = 148 * 8;
-  // Cutting costs a join, so it has to be worth 2 us at least: where every SM has a block anyway that is a tile of 2048 keys.
-  // Tables no wider than min_cut also save the join's launch.
+  // Cutting costs a join, so it has to be worth 2 us at least: where every SM has a block anyway that is a tile of 2048 keys
+  // (one token each behind 1500, 16 / 8 heads, 40 sequences: 51.8 us against 57.0 with 512; 20 of them 24.5 against 25.3; 4 of
+  // them, cut, 11.5 against 16.8 uncut).  Tables no wider than min_cut also save the join's launch.
   const bool busy = (long long)n_seq * hkv >= 148;
   s->min_cut = busy ? 2048 : 512;
   const bool few = (long long)max_q * g <= 32 && g <= 16;
@@ -530,8 +531,11 @@ bool paged_plan_shape(int n_seq, int total_q, int max_q, int hq, int hkv, int dh
     return true;
   }
   if (g > 64) return false;
-  // 64 rows a block use the FMA units best (16 are bound by shared-memory reads); 16 spread a small call over the SMs
-  const bool small = few || (g <= 16 && ((long long)total_q * g / 64 + n_seq) * hkv < 148 * 2);
+  // 64 rows a block use the FMA units best (16 are bound by shared-memory reads): 256 tokens behind 4096, 16 heads, 376 us
+  // against 716.  16 spread a call of few short sequences over the SMs and fill their tiles: 16 documents of 32 tokens, 4 heads
+  // of 64, 6.7 us against 9.9, 48 of them 11.6 against 10.3; 8 of 40 tokens, 16 heads, 17.8 against 14.1, 4 of them 12.6
+  // against 14.0.  (fp32; how deep the cache is, which would decide the cases between, is not known here.)
+  const bool small = few || (g <= 16 && (long long)max_q * g <= 96 && ((long long)total_q * g / 64 + n_seq) * hkv < 128);
   s->kind = kPagedSimt, s->rows = small ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 256, s->slots = 148 * 2;
   s->ns_key = small ? 10.f : 40.f, s->ns_key_block = 0.f, s->ns_item = 2000.f, s->ns_part = 1000.f, s->ns_join = 2500.f;
   return true;

@@ -101,6 +101,38 @@ def test_append(P, n, page, cached, new, in_place):
     assert np.array_equal(got["free"], free)
 
 
+def test_append_of_many_rows_captured_and_replayed(P):
+    """More rows than one cluster writes: the rows come from a second kernel, in a graph too, also when the call is refused."""
+    n, page, total = 700, 32, 80000
+    rng, kv, add, (table, free, n_free, pool) = append_inputs(n, page, (0, 300), (0, 220))
+    assert int(add.sum()) <= total
+    lens, kvd, out, nf, nfo, t, f = i32(add), i32(kv), i32(np.zeros(n)), i32([n_free]), i32([0]), i32(table), i32(free)
+    cu, pos, slot, err = i32(np.zeros(n + 1)), i32(np.zeros(total)), i32(np.zeros(total)), err_word()
+    run = lambda: P.ops.prism_op_page_append(lens, kvd, out, page, pool, t, f, nf, nfo, cu, pos, slot, err)
+    run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for new in (add, np.roll(np.minimum(add, 40), 3), np.where(np.arange(n) == 650, -1, add), add):
+        for x in (t, cu, pos, slot, out):
+            x.fill_(-9)
+        t.copy_(i32(table))
+        lens.copy_(i32(new))
+        err.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        if new.min() < 0:
+            assert int(err.item()) == 2 and not cu.any() and not pos.any() and (slot == -1).all()
+            assert torch.equal(t, i32(table)) and torch.equal(out, kvd) and torch.equal(nfo, nf)
+            continue
+        want = append(kv_len=kv, len_new=new, page=page, table=table, free=free, n_free=n_free, total=total)
+        assert int(err.item()) == 0
+        for got, w in zip((out, t, nfo, cu, pos, slot), want):
+            assert np.array_equal(got.cpu().numpy().ravel(), np.asarray(w).ravel())
+    g.reset()
+
+
 def test_append_uses_the_last_page_and_no_sequences(P):
     got, err = call_append(P, np.array([0, 16]), np.array([16, 1]), 16, 3, np.array([[-1, -1], [2, -1]]), np.array([0, 1, 7]), 2, 17)
     assert err == 0 and got["nf"][0] == 0 and got["table"].tolist() == [[1, -1], [2, 0]] and got["slot"][-1] == 0
