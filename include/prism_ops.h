@@ -197,7 +197,8 @@ typedef struct {
  * kv_len_out may be kv_len_in and n_free_out may be n_free_in.  Refused as a whole, with an error bit: a negative length, a
  * sequence beyond max_pages, more rows than `total`, too few free pages; then kv_len_out = kv_len_in, *n_free_out =
  * *n_free_in, cu_q = 0, every slot -1 and the table is untouched.  A page id outside [0, num_pages) sets bit 16, is
- * entered as -1 and its rows get slot -1. */
+ * entered as -1 and its rows get slot -1.  A page that several sequences read has to be full before they append: the
+ * tokens behind a sequence's last one go into its own last page. */
 PRISM_API int prism_op_page_append(const int32_t* len_new, const int32_t* kv_len_in, int32_t* kv_len_out, int32_t n_seq,
                                    int32_t page_size, int32_t num_pages, int32_t max_pages, int64_t table_stride,
                                    int32_t* block_table, const int32_t* free_pages, const int32_t* n_free_in, int32_t* n_free_out,

@@ -9,6 +9,9 @@ synthetic operands, one JSON line per run.  Also the small-case driver for profi
     python -m paper_2510_15620_b200.microbench --op dequant --n 12288 --k 4096          (W4 -> bf16, group 128)
     python -m paper_2510_15620_b200.microbench --op probe|route --seqs 1000                (score probe; prune decision)
     python -m paper_2510_15620_b200.microbench --op attention --head-dim 64 --hq 16 --hkv 16 --causal 0
+    python -m paper_2510_15620_b200.microbench --op attention_paged --seqs 100 --len-lo 1 --len-hi 1 --cached-lo 500 --cached-hi 16384
+    python -m paper_2510_15620_b200.microbench --op rope_paged --rows 35200            (norm, rotation, cache write)
+    python -m paper_2510_15620_b200.microbench --op page_append|page_release --seqs 1000
 """
 from __future__ import annotations
 
@@ -39,9 +42,68 @@ def _time(fn, iters, warmup, flush):
     return float(np.median(ms)), float(np.min(ms))
 
 
+def _paged(a, out, rnd, flush):
+    """The paged cache: len-lo .. len-hi new tokens a sequence behind cached-lo .. cached-hi, pages scattered over the pool."""
+    rng = np.random.default_rng(0)
+    t = lambda v: torch.from_numpy(np.ascontiguousarray(v, dtype=np.int32)).cuda()
+    n, dh, page, width = a.seqs, a.head_dim, a.page, (a.hq + 2 * a.hkv) * a.head_dim
+    pages = lambda tokens: -(-tokens // page)
+    err, bf16 = t([0]), torch.bfloat16
+    cached = rng.integers(a.cached_lo, a.cached_hi + 1, size=n)
+    new = rng.integers(a.len_lo, a.len_hi + 1, size=n)
+    kv = cached + new
+    if a.op == "rope_paged":
+        pool = pages(a.rows)
+        qkv, q = rnd(a.rows, width).to(bf16), torch.empty(a.rows, a.hq * dh, dtype=bf16, device="cuda")
+        k, v = (torch.empty(pool, a.hkv, page, dh, dtype=bf16, device="cuda") for _ in range(2))
+        order = rng.permutation(pool)
+        row = np.arange(a.rows)
+        pos, slot, gain = t(row % 512), t(order[row // page] * page + row % page), torch.ones(dh, dtype=bf16, device="cuda")
+        fn = lambda: ops.prism_op_qknorm_rope_paged(qkv, PRISM_BF16, pos, slot, a.hq, a.qk_norm, gain, gain, 1e-6, 1e6, q, k, v, err)
+        med, best = _time(fn, a.iters, a.warmup, flush)
+        out.update(rows=a.rows, head_dim=dh, ms=med, ms_min=best, gbs=a.rows * width * 4.0 / med / 1e6, err=int(err.item()))
+        return
+    pool, max_pages = int(pages(kv).sum()), int(pages(kv).max())
+    free = rng.permutation(pool)
+    table, at = np.full((n, max_pages), -1), 0
+    for s, tokens in enumerate(cached if a.op == "page_append" else kv):
+        table[s, :pages(tokens)] = free[at:at + pages(tokens)]
+        at += pages(tokens)
+    tab, kvd = t(table), t(cached if a.op == "page_append" else kv)
+    if a.op == "page_append":
+        left, n_free = t(np.roll(free, -at)), t([pool - at])
+        total = int(new.sum())
+        lens, kv_out, cu, pos, slot, nf = t(new), t(np.zeros(n)), t(np.zeros(n + 1)), t(np.zeros(total)), t(np.zeros(total)), t([0])
+        fn = lambda: ops.prism_op_page_append(lens, kvd, kv_out, page, pool, tab, left, n_free, nf, cu, pos, slot, err)
+        med, best = _time(fn, a.iters, a.warmup, flush)
+        out.update(seqs=n, rows=total, ms=med, ms_min=best, err=int(err.item()))
+    elif a.op == "page_release":
+        keep = np.sort(rng.choice(n, size=max(1, n // 3), replace=False))
+        stack, n_free, nf, kv_out, tab_out = t(np.zeros(pool)), t([0]), t([0]), t(np.zeros(n)), torch.empty_like(tab)
+        keep_d = t(keep)
+        fn = lambda: ops.prism_op_page_release(keep_d, kvd, kv_out, page, pool, 0, tab, tab_out, stack, n_free, nf, err)
+        med, best = _time(fn, a.iters, a.warmup, flush)
+        out.update(seqs=n, kept=len(keep), pages_freed=int(nf.item()), ms=med, ms_min=best, err=int(err.item()))
+    else:
+        cu = np.concatenate([[0], np.cumsum(new)])
+        rows, max_q = int(cu[-1]), int(new.max())
+        q, o = rnd(rows, a.hq * dh).to(bf16), torch.empty(rows, a.hq * dh, dtype=bf16, device="cuda")
+        k, v = (rnd(pool, a.hkv, page, dh).to(bf16) for _ in range(2))
+        pb, wb = ops.prism_op_attention_paged_bytes(n, rows, max_q, a.hq, a.hkv, dh, PRISM_BF16, a.impl)
+        plan, ws = (torch.empty(b, dtype=torch.uint8, device="cuda") for b in (pb, wb))
+        ops.prism_op_attention_paged_plan(t(cu), kvd, rows, max_q, a.hq, a.hkv, dh, PRISM_BF16, a.causal, plan, err, a.impl)
+        fn = lambda: ops.prism_op_attention_paged(q, k, v, tab, plan, n, max_q, a.hq, PRISM_BF16, o, ws, err, a.impl)
+        med, best = _time(fn, a.iters, a.warmup, flush)
+        seen = new * kv - (new * (new - 1) / 2 if a.causal else 0)   # (query, key) pairs
+        out.update(seqs=n, rows=rows, keys=int(kv.sum()), causal=a.causal, head_dim=dh, ms=med, ms_min=best,
+                   tflops=4.0 * float(seen.sum()) * a.hq * dh / med / 1e9,
+                   gbs=(4.0 * float(kv.sum()) * a.hkv * dh + 4.0 * rows * a.hq * dh) / med / 1e6, err=int(err.item()))
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("--op", required=True, choices=["gemm", "qkv_rope", "attention", "rmsnorm", "rope", "compact", "gemm_bias", "layernorm", "dequant", "probe", "route"])
+    ap.add_argument("--op", required=True, choices=["gemm", "qkv_rope", "attention", "rmsnorm", "rope", "compact", "gemm_bias", "layernorm", "dequant", "probe", "route",
+                                                   "attention_paged", "rope_paged", "page_append", "page_release"])
     ap.add_argument("--head-dim", type=int, default=128)
     ap.add_argument("--m", type=int, default=35200)
     ap.add_argument("--n", type=int, default=4096)
@@ -53,6 +115,9 @@ def main():
     ap.add_argument("--seqs", type=int, default=100)
     ap.add_argument("--len-lo", type=int, default=160)
     ap.add_argument("--len-hi", type=int, default=544)
+    ap.add_argument("--cached-lo", type=int, default=32)
+    ap.add_argument("--cached-hi", type=int, default=32)
+    ap.add_argument("--page", type=int, default=16)
     ap.add_argument("--hq", type=int, default=16)
     ap.add_argument("--hkv", type=int, default=8)
     ap.add_argument("--causal", type=int, default=1)
@@ -192,6 +257,8 @@ def main():
         med, best = _time(fn, a.iters, a.warmup, flush)
         out.update(rows=a.rows, ms=med, ms_min=best, gbs=a.rows * (a.hq + a.hkv) * dh * 4.0 / med / 1e6,
                    note="includes the op wrapper's table build and sync")
+    elif a.op in ("attention_paged", "rope_paged", "page_append", "page_release"):
+        _paged(a, out, rnd, flush)
     else:
         n = a.seqs
         rng = np.random.default_rng(0)
