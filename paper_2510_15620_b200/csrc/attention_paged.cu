@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include "paged.cuh"
+#include "tc_common.cuh"
 
 namespace prism {
 namespace {
@@ -283,11 +284,18 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedPlanHeader want, const 
 // Bound by FMA issue and shared-memory reads at R = 64, by latency in small calls, by reading the cache at R = 16.
 constexpr int kKeys = 64;
 
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+// four neighbouring elements as two pairs of floats, what an FMA on pairs takes
+struct Quad {
+  uint64_t a, b;
+};
+__device__ __forceinline__ Quad load4(const float* p) {
+  const ulonglong2 u = *reinterpret_cast<const ulonglong2*>(p);
+  return Quad{u.x, u.y};
+}
+__device__ __forceinline__ Quad load4(const __nv_bfloat16* p) {
   const uint2 u = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xffff0000u));
+  return Quad{tc::f2_pack(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u)),
+              tc::f2_pack(__uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u))};
 }
 __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
@@ -374,14 +382,14 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
     // rows of this thread: ty + 16 i.  lim: keys below it are visible
     int lim[RT];
     float m[RT], l[RT];
-    float4 o[RT][NC];
+    Quad o[RT][NC];
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
       const int r = ty + 16 * i, tok = r / group;
       lim[i] = tok < it.n_tok ? (causal ? min(it.k1, it.pos0 + tok + 1) : it.k1) : 0;
       m[i] = -INFINITY, l[i] = 0.f;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int c = 0; c < NC; ++c) o[i][c] = Quad{0, 0};
     }
     for (int t = 0; t < n_tiles; ++t) {
       const int k0 = it.k0 + t * kKeys;
@@ -390,14 +398,14 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
       if (t + 1 < n_tiles) locate(t + 1);
       copies_wait<1>();  // keys (and queries); the values are still on their way
       __syncthreads();
-      float s[RT][4];
+      uint64_t s2[RT][4];  // sums over even and over odd elements
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+        for (int j = 0; j < 4; ++j) s2[i][j] = 0;
 #pragma unroll 4
       for (int c = 0; c < dh; c += 4) {
-        float4 qa[RT], kb[4];
+        Quad qa[RT], kb[4];
 #pragma unroll
         for (int i = 0; i < RT; ++i) qa[i] = load4(s_q + (ty + 16 * i) * ld + c);
 #pragma unroll
@@ -406,15 +414,17 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
         for (int i = 0; i < RT; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            s[i][j] += qa[i].x * kb[j].x + qa[i].y * kb[j].y + qa[i].z * kb[j].z + qa[i].w * kb[j].w;
+            s2[i][j] = tc::f2_fma(qa[i].b, kb[j].b, tc::f2_fma(qa[i].a, kb[j].a, s2[i][j]));
       }
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        float mx = -INFINITY;
+        float mx = -INFINITY, s[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          s[i][j] = k0 + tx + 16 * j < lim[i] ? s[i][j] * scale_log2 : -INFINITY;
-          mx = fmaxf(mx, s[i][j]);
+          float even, odd;
+          tc::f2_unpack(s2[i][j], even, odd);
+          s[j] = k0 + tx + 16 * j < lim[i] ? (even + odd) * scale_log2 : -INFINITY;
+          mx = fmaxf(mx, s[j]);
         }
 #pragma unroll
         for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
@@ -424,13 +434,16 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float p = exp2f(s[i][j] - ref);
+          const float p = exp2f(s[j] - ref);
           sum += p;
           s_p[(ty + 16 * i) * (kKeys + 4) + tx + 16 * j] = p;
         }
         l[i] = l[i] * f + sum;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) o[i][c].x *= f, o[i][c].y *= f, o[i][c].z *= f, o[i][c].w *= f;
+        for (int c = 0; c < NC; ++c) {
+          const uint64_t ff = tc::f2_pack(f, f);
+          o[i][c] = Quad{tc::f2_mul(o[i][c].a, ff), tc::f2_mul(o[i][c].b, ff)};
+        }
       }
       copies_wait<0>();
       __syncthreads();  // the values are there, the keys have been read, the next tile's addresses are known
@@ -446,11 +459,12 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
           if (col < dh) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float4 v = load4(s_v + (kk + e) * ld + col);
+              const Quad v = load4(s_v + (kk + e) * ld + col);
 #pragma unroll
               for (int i = 0; i < RT; ++i) {
                 const float w = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
-                o[i][c].x += w * v.x, o[i][c].y += w * v.y, o[i][c].z += w * v.z, o[i][c].w += w * v.w;
+                const uint64_t ww = tc::f2_pack(w, w);
+                o[i][c] = Quad{tc::f2_fma(ww, v.a, o[i][c].a), tc::f2_fma(ww, v.b, o[i][c].b)};
               }
             }
           }
@@ -471,7 +485,9 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const int col = tx * 4 + 64 * c;
-        float4 v = o[i][c];
+        float4 v;
+        tc::f2_unpack(o[i][c].a, v.x, v.y);
+        tc::f2_unpack(o[i][c].b, v.z, v.w);
         if (col >= dh) continue;
         if (p) {
           *reinterpret_cast<float4*>(p + ((long long)(col >> 2) * R + r) * 4) = v;
