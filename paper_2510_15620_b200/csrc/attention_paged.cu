@@ -281,7 +281,11 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedPlanHeader want, const 
 // type: the values of a tile load under its scores, the next tile's keys under its second product, and the addresses (one
 // page-table read per key) are worked out a tile ahead.  Rows are padded by 16 bytes so that neighbouring rows start in
 // different banks.
-// Bound by FMA issue and shared-memory reads at R = 64, by latency in small calls, by reading the cache at R = 16.
+// Bound by FMA issue and shared-memory reads at R = 64 (both about 60 % busy), by latency in small calls, by reading the cache
+// at R = 16.
+// Measured, fp32, 16 query and 8 key/value heads of 128: 20 x 352 tokens behind 512 1174 us (33.8 TFLOP/s of causal pairs; single
+// FMAs instead of FMAs on pairs of floats 1566, one block an SM with the probabilities in memory of their own 1372), 1024 tokens
+// behind 8192 2345 us (3026, 2645); 16 documents of 32 tokens, 4 heads of 64, 6.7 us.
 constexpr int kKeys = 64;
 
 // four neighbouring elements as two pairs of floats, what an FMA on pairs takes
@@ -312,16 +316,24 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// shared memory: queries, values, keys, probabilities, key addresses.  At 64 rows the probabilities go over the keys, so that
+// two blocks fit on an SM up to head_dim 128.
+template <typename T>
+__host__ __device__ constexpr int simt_keys(int rows, int dh) {
+  const int k = kKeys * (dh * (int)sizeof(T) + 16), p = rows * (kKeys + 4) * 4;
+  return rows != 64 ? k + p : k > p ? k : p;
+}
 template <typename T>
 __host__ __device__ constexpr int simt_smem(int rows, int dh) {
-  return (rows + 2 * kKeys) * (dh * (int)sizeof(T) + 16) + rows * (kKeys + 4) * 4 + 2 * kKeys * 8;
+  return (rows + kKeys) * (dh * (int)sizeof(T) + 16) + simt_keys<T>(rows, dh) + 2 * kKeys * 8;
 }
 
 template <typename T, int R, int NC>
-__global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, float scale_log2) {
+__global__ void __launch_bounds__(256, R == 64 && NC == 4 ? 1 : 2) k_paged_simt(PagedAttnArgs a, int shift, float scale_log2) {
   pdl_sync();
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int RT = R / 16;
+  constexpr bool kOver = R == 64;  // probabilities over the keys
   const PagedPlanHeader* hd = static_cast<const PagedPlanHeader*>(a.plan);
   const int hkv = a.c.hkv, dh = a.c.dh, group = a.hq / hkv;
   // the grid is not larger than the list's room, so the first item can be fetched beside the header
@@ -335,10 +347,11 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
   const int ld = dh + 16 / (int)sizeof(T);          // elements from row to row
   const int pieces = dh * (int)sizeof(T) / 16;      // 16-byte pieces of a row
   T* s_q = reinterpret_cast<T*>(smem);
-  T* s_k = s_q + R * ld;
-  T* s_v = s_k + kKeys * ld;
-  float* s_p = reinterpret_cast<float*>(s_v + kKeys * ld);
-  long long* s_at = reinterpret_cast<long long*>(s_p + R * (kKeys + 4));  // [2][64] element offset of each key's row, or -1
+  T* s_v = s_q + R * ld;
+  T* s_k = s_v + kKeys * ld;
+  float* s_p = reinterpret_cast<float*>(kOver ? s_k : s_k + kKeys * ld);
+  // [2][64] element offset of each key's row, or -1
+  long long* s_at = reinterpret_cast<long long*>(reinterpret_cast<unsigned char*>(s_k) + simt_keys<T>(R, dh));
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   for (int work = blockIdx.x; work < total; work += gridDim.x) {
     const int h = work % hkv;
@@ -393,7 +406,8 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
     }
     for (int t = 0; t < n_tiles; ++t) {
       const int k0 = it.k0 + t * kKeys;
-      if (t > 0) __syncthreads();  // every thread is through with the previous tile's values
+      if (t > 0) __syncthreads();  // every thread is through with the previous tile's values and probabilities
+      if (kOver && t > 0) fetch(s_k, a.c.k, t);
       fetch(s_v, a.c.v, t);
       if (t + 1 < n_tiles) locate(t + 1);
       copies_wait<1>();  // keys (and queries); the values are still on their way
@@ -416,6 +430,7 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
           for (int j = 0; j < 4; ++j)
             s2[i][j] = tc::f2_fma(qa[i].b, kb[j].b, tc::f2_fma(qa[i].a, kb[j].a, s2[i][j]));
       }
+      if (kOver) __syncthreads();  // the keys have been read
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
         float mx = -INFINITY, s[4];
@@ -447,7 +462,7 @@ __global__ void __launch_bounds__(256) k_paged_simt(PagedAttnArgs a, int shift, 
       }
       copies_wait<0>();
       __syncthreads();  // the values are there, the keys have been read, the next tile's addresses are known
-      if (t + 1 < n_tiles) fetch(s_k, a.c.k, t + 1);
+      if (!kOver && t + 1 < n_tiles) fetch(s_k, a.c.k, t + 1);
       const int nk = min(kKeys, it.k1 - k0);
       for (int kk = 0; kk < nk; kk += 4) {  // (keys of the last four beyond nk have p = 0 and zero values)
         float4 p[RT];
