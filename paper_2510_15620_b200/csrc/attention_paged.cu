@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedPlanHeader want, const 
 // at R = 16.
 // Measured, fp32, 16 query and 8 key/value heads of 128: 20 x 352 tokens behind 512 1174 us (33.8 TFLOP/s of causal pairs; single
 // FMAs instead of FMAs on pairs of floats 1566, one block an SM with the probabilities in memory of their own 1372), 1024 tokens
-// behind 8192 2345 us (3026, 2645); 16 documents of 32 tokens, 4 heads of 64, 6.7 us.
+// behind 8192 2345 us (3026, 2645); 16 documents of 32 tokens, 4 heads of 64, 6.5 us.
 constexpr int kKeys = 64;
 
 // four neighbouring elements as two pairs of floats, what an FMA on pairs takes
@@ -316,24 +316,24 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// shared memory: queries, values, keys, probabilities, key addresses.  At 64 rows the probabilities go over the keys, so that
-// two blocks fit on an SM up to head_dim 128.
+// Shared memory: queries, values, keys, probabilities, key addresses.  `over`: the probabilities go over the keys, so that two
+// blocks of 64 rows fit on an SM up to head_dim 128; the next keys are then fetched after the second product only, which the
+// other block covers.
 template <typename T>
-__host__ __device__ constexpr int simt_keys(int rows, int dh) {
+__host__ __device__ constexpr int simt_keys(int rows, int dh, bool over) {
   const int k = kKeys * (dh * (int)sizeof(T) + 16), p = rows * (kKeys + 4) * 4;
-  return rows != 64 ? k + p : k > p ? k : p;
+  return !over ? k + p : k > p ? k : p;
 }
 template <typename T>
-__host__ __device__ constexpr int simt_smem(int rows, int dh) {
-  return (rows + kKeys) * (dh * (int)sizeof(T) + 16) + simt_keys<T>(rows, dh) + 2 * kKeys * 8;
+__host__ __device__ constexpr int simt_smem(int rows, int dh, bool over) {
+  return (rows + kKeys) * (dh * (int)sizeof(T) + 16) + simt_keys<T>(rows, dh, over) + 2 * kKeys * 8;
 }
 
-template <typename T, int R, int NC>
-__global__ void __launch_bounds__(256, R == 64 && NC == 4 ? 1 : 2) k_paged_simt(PagedAttnArgs a, int shift, float scale_log2) {
+template <typename T, int R, int NC, bool kOver>
+__global__ void __launch_bounds__(256, R == 16 || kOver ? 2 : 1) k_paged_simt(PagedAttnArgs a, int shift, float scale_log2) {
   pdl_sync();
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int RT = R / 16;
-  constexpr bool kOver = R == 64;  // probabilities over the keys
   const PagedPlanHeader* hd = static_cast<const PagedPlanHeader*>(a.plan);
   const int hkv = a.c.hkv, dh = a.c.dh, group = a.hq / hkv;
   // the grid is not larger than the list's room, so the first item can be fetched beside the header
@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(256, R == 64 && NC == 4 ? 1 : 2) k_paged_simt(
   T* s_k = s_v + kKeys * ld;
   float* s_p = reinterpret_cast<float*>(kOver ? s_k : s_k + kKeys * ld);
   // [2][64] element offset of each key's row, or -1
-  long long* s_at = reinterpret_cast<long long*>(reinterpret_cast<unsigned char*>(s_k) + simt_keys<T>(R, dh));
+  long long* s_at = reinterpret_cast<long long*>(reinterpret_cast<unsigned char*>(s_k) + simt_keys<T>(R, dh, kOver));
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   for (int work = blockIdx.x; work < total; work += gridDim.x) {
     const int h = work % hkv;
@@ -522,16 +522,16 @@ int log2_of(int x) {
   return s;
 }
 
-template <typename T, int R, int NC>
+template <typename T, int R, int NC, bool kOver>
 cudaError_t simt_launch(const PagedAttnArgs& a, int grid, cudaStream_t st) {
   static std::atomic<unsigned long long> set;
-  const int smem = simt_smem<T>(R, a.c.dh);
-  if (cudaError_t e = ensure_dynamic_smem(k_paged_simt<T, R, NC>, simt_smem<T>(R, 64 * NC), set)) return e;
+  const int smem = simt_smem<T>(R, a.c.dh, kOver);
+  if (cudaError_t e = ensure_dynamic_smem(k_paged_simt<T, R, NC, kOver>, simt_smem<T>(R, 64 * NC, kOver), set)) return e;
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)a.c.dh);
-  k_paged_simt<T, R, NC><<<grid, 256, smem, st>>>(a, log2_of(a.c.page_size), scale_log2);
+  k_paged_simt<T, R, NC, kOver><<<grid, 256, smem, st>>>(a, log2_of(a.c.page_size), scale_log2);
   return cudaGetLastError();
 }
-static_assert(simt_smem<float>(64, 256) <= 232448, "exceeds the shared memory one block may have");
+static_assert(simt_smem<float>(64, 256, false) <= 232448, "exceeds the shared memory one block may have");
 
 }  // namespace
 
@@ -562,10 +562,10 @@ bool paged_plan_shape(int n_seq, int total_q, int max_q, int hq, int hkv, int dh
     return true;
   }
   if (g > 64) return false;
-  // 64 rows a block use the FMA units best (16 are bound by shared-memory reads): 256 tokens behind 4096, 16 heads, 376 us
-  // against 716.  16 spread a call of few short sequences over the SMs and fill their tiles: 16 documents of 32 tokens, 4 heads
-  // of 64, 6.7 us against 9.9, 48 of them 11.6 against 10.3; 8 of 40 tokens, 16 heads, 17.8 against 14.1, 4 of them 12.6
-  // against 14.0.  (fp32; how deep the cache is, which would decide the cases between, is not known here.)
+  // 64 rows a block use the FMA units best (16 are bound by shared-memory reads): 256 tokens behind 4096, 16 heads, 298 us
+  // against 733.  16 spread a call of few short sequences over the SMs and fill their tiles: 16 documents of 32 tokens, 4 heads
+  // of 64, 6.5 us against 9.8, 48 of them 13.2 against 10.1; 8 of 40 tokens, 16 heads, 17.1 against 13.3, 4 of them 12.4
+  // against 13.2.  (fp32; how deep the cache is, which would decide the cases between, is not known here.)
   const bool small = few || (g <= 16 && (long long)max_q * g <= 96 && ((long long)total_q * g / 64 + n_seq) * hkv < 128);
   s->kind = kPagedSimt, s->rows = small ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 256, s->slots = 148 * 2;
   s->ns_key = small ? 10.f : 40.f, s->ns_key_block = 0.f, s->ns_item = 2000.f, s->ns_part = 1000.f, s->ns_join = 2500.f;
@@ -610,14 +610,20 @@ cudaError_t launch_paged_join(const PagedAttnArgs& a, const PagedPlanShape& s, i
 
 cudaError_t launch_paged_simt(const PagedAttnArgs& a, const PagedPlanShape& s, int grid, cudaStream_t st) {
   const int dh = a.c.dh;
-#define PRISM_SIMT(T)                                                                     \
-  (s.rows == 16 ? (dh <= 64    ? simt_launch<T, 16, 1>(a, grid, st)                       \
-                   : dh <= 128 ? simt_launch<T, 16, 2>(a, grid, st)                       \
-                               : simt_launch<T, 16, 4>(a, grid, st))                      \
-                : (dh <= 64    ? simt_launch<T, 64, 1>(a, grid, st)                       \
-                   : dh <= 128 ? simt_launch<T, 64, 2>(a, grid, st)                       \
-                               : simt_launch<T, 64, 4>(a, grid, st)))
-  return a.c.dtype == 1 ? PRISM_SIMT(__nv_bfloat16) : PRISM_SIMT(float);
+  // `most`: blocks the lengths may ask for.  Where no SM can get two (or fit two: above head_dim 128), the probabilities keep
+  // memory of their own: 4 x 40 fp32 tokens behind 1000, 8 query and 2 key/value heads of 128, 53 us against 82; 256 tokens
+  // behind 4096, 16 and 8 heads, 376 against 298.
+  const long long keys = (long long)a.max_pages * a.c.page_size;
+  const long long pieces = keys > s.min_cut ? (keys + s.min_piece - 1) / s.min_piece : 1;
+  const long long most = ((long long)a.total_q / s.tokens + a.n_seq) * a.c.hkv * pieces;
+  const bool over = most > 148;
+#define PRISM_SIMT(T, R, OVER)                                       \
+  (dh <= 64    ? simt_launch<T, R, 1, OVER>(a, grid, st)             \
+   : dh <= 128 ? simt_launch<T, R, 2, OVER>(a, grid, st)             \
+               : simt_launch<T, R, 4, false>(a, grid, st))
+#define PRISM_SIMT_ROWS(T) (s.rows == 16 ? PRISM_SIMT(T, 16, false) : over ? PRISM_SIMT(T, 64, true) : PRISM_SIMT(T, 64, false))
+  return a.c.dtype == 1 ? PRISM_SIMT_ROWS(__nv_bfloat16) : PRISM_SIMT_ROWS(float);
+#undef PRISM_SIMT_ROWS
 #undef PRISM_SIMT
 }
 
