@@ -239,7 +239,7 @@ PRISM_API int prism_op_qknorm_rope_paged(const void* qkv, int64_t qkv_stride, co
  * prism_op_attention_paged_plan reads cu_q and kv_len and writes the plan; prism_op_attention_paged then takes the same
  * n_seq, total_q (rows of q), max_q_len (no sequence has more new rows), heads, dtype and impl.
  * prism_op_attention_paged_bytes (host only) gives the sizes of plan and workspace; the workspace is scratch of one call
- * and may be NULL when max_pages * page_size <= 512.
+ * and may be NULL when max_pages * page_size <= 128.
  * impl: PRISM_IMPL_AUTO = tensor cores for bf16 at head_dim 64 and 128 (Hq/Hkv <= 128): warp-level MMA with the cache streamed
  * through shared memory when max_q_len * Hq/Hkv <= 32 and Hq/Hkv <= 16, else tcgen05; CUDA cores otherwise (Hq/Hkv <= 64).
  * PRISM_IMPL_SIMT = CUDA cores.  Results do not depend on other sequences' contents; they may differ in rounding between plans

@@ -17,7 +17,7 @@ constexpr int kSearch = 1024;
 // ------------------------------------------------------------------------------------------------ work list
 // One block.  Tiles of s.tokens tokens; a tile whose keys are more than `piece` is cut into equal pieces so that few long
 // sequences still occupy every SM.  Up to kSearch tiles, 32 warps weigh 32 piece lengths against each other (no cut, the
-// longest tile over 2, 3, ... 32): waves of blocks times a mean piece, plus what the longest piece exceeds it by.  Beyond that
+// longest tile over 2, 3, ... 16, then in steps of a fifth up to 256): waves of blocks times a mean piece, plus what the longest piece exceeds it by.  Beyond that
 // the SMs are busy anyway and only tiles far longer than the others are cut.  No piece is shorter than the launch's total
 // (keys x heads) over s.target, hence the bounds of paged_plan_bounds.  Tiles are listed from the last to the first: under
 // causal attention a sequence's last tile has the most keys, and the launch should end on light ones.
@@ -118,7 +118,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const int* __restri
   if (n_tiles <= kSearch) {
     longest = __reduce_max_sync(0xffffffffu, s_longest[tid & 31]);
     const int j = tid >> 5, lane = tid & 31;
-    unsigned len = j == 0 ? 0x7fffffffu : (((unsigned)longest + j) / (j + 1) + sh.piece_unit - 1) / sh.piece_unit * sh.piece_unit;
+    const unsigned over = j < 16 ? j + 1 : (unsigned)(16.f * exp2f((j - 15) * 0.25f));  // 1, 2, ... 16, 19, 22, ... 256
+    unsigned len = j == 0 ? 0x7fffffffu : (((unsigned)longest + over - 1) / over + sh.piece_unit - 1) / sh.piece_unit * sh.piece_unit;
     if (len < piece) len = (unsigned)min(piece, 0x7fffffffll);
     unsigned items_n = 0, parts_n = 0;
     for (int t = lane; t < n_tiles; t += 32) {
@@ -516,6 +517,251 @@ __global__ void __launch_bounds__(256, R == 16 || kOver ? 2 : 1) k_paged_simt(Pa
   }
 }
 
+// ------------------------------------------------------------------------------------------------ few rows on CUDA cores
+// The same for single tokens and the like, at most 8 query rows a sequence and key/value head: every key and value is used for
+// at most 8 rows, so what counts is how they are fetched.  One warp per unit of work, nothing shared between warps: a block is a
+// warp, as many of them per SM as their shared memory allows, and long key ranges come cut into pieces by the work list.  The warp
+// takes 32 keys at a time.  Scores: a lane owns a key, queries are broadcast, so a key crosses the shared-memory port once (in
+// the kernel above once per pair of rows).  Output: a lane owns four columns (groups of lanes share the keys where a row has less
+// than 128 columns), probabilities are broadcast.  Every lane fetches its key's row with one bulk copy; the next keys load
+// under the softmax and the second product, the next values under the next scores.  RL: rows, rounded up to 4 or 8; NCH: sets
+// of four columns of a lane.
+// Bound by the latency of a step (32 keys) while the SM's memory holds 5 (head_dim 128) or 10 (64) fp32 warps.
+// Measured, fp32, one token each, against 16 rows a block of the kernel above: 1 sequence behind 19 k, 28 query and 4 key/value
+// heads of 128, 75 us (187); 6 behind 6-12 k, 16 and 8 heads of 64, 71 us, 3.4 TB/s (199); 135 of 10, 16 and 16 heads of 64, 13 us
+// (45); 1 behind 9, 32 and 8 heads of 64, 7.4 us (6.4); 1 of two tokens behind 8-241, 8 and 1 heads of 64, 12 us (6.3).  With 16 rows a warp is too slow: 2 sequences of two tokens behind 31, 28
+// and 4 heads of 128, 25 us (9.5).  Row pieces of 16 bytes fetched by asynchronous copies of all lanes: 5-30 % slower.
+constexpr int kFewKeys = 32;
+
+template <typename T>
+__host__ __device__ constexpr int few_smem(int rl, int dh) {
+  return 2 * kFewKeys * (dh * (int)sizeof(T) + 16) + rl * dh * 4 + kFewKeys * (rl + 4) * 4 + 32;
+}
+// One row of the cache to shared memory (addresses and size multiples of 16 bytes); its bytes are counted by the barrier.
+__device__ __forceinline__ void copy_row(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+template <typename T, int RL, int NCH>
+__global__ void __launch_bounds__(32) k_paged_few(PagedAttnArgs a, int shift, float scale_log2) {
+  pdl_sync();
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int E = 16 / (int)sizeof(T), PP = RL + 4;  // elements of 16 bytes; probabilities from key to key
+  const PagedPlanHeader* hd = static_cast<const PagedPlanHeader*>(a.plan);
+  const int hkv = a.c.hkv, dh = a.c.dh, group = a.hq / hkv, lane = threadIdx.x;
+  // the grid is not larger than the list's room, so the first item can be fetched beside the header
+  PagedItem it = paged_item_raw(hd, blockIdx.x / hkv);
+  if (hd->kind != kPagedFew || hd->hq != a.hq || hd->hkv != hkv || hd->dh != dh || hd->total_q != a.total_q ||
+      hd->n_seq != a.n_seq || hd->max_q != a.max_q) {
+    if (lane == 0 && blockIdx.x == 0) atomicOr(a.err, kErrBadOffsets);
+    return;
+  }
+  const int total = hd->n_items * hkv, causal = hd->causal;
+  const int ld = dh + E;
+  const uint32_t row_bytes = (uint32_t)dh * sizeof(T);
+  T* s_k = reinterpret_cast<T*>(smem);
+  T* s_v = s_k + kFewKeys * ld;
+  float* s_q = reinterpret_cast<float*>(s_v + kFewKeys * ld);
+  float* s_p = s_q + RL * dh;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_p + kFewKeys * PP);
+  const uint32_t b_k = tc::smem_u32(bars), b_v = b_k + 8;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 2);
+  if (lane == 0) {
+    tc::mbar_init(b_k, 1);
+    tc::mbar_init(b_v, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  uint32_t done = 0;  // tiles this warp has been through
+  bool ok = true;
+  // columns 4 chunk .. + 3 of the output (and 128 further on), keys grp, grp + groups, ... of a tile
+  const int chunks = dh / 4, groups = NCH == 1 ? 32 / chunks : 1, grp = NCH == 1 ? lane / chunks : 0, chunk = lane - grp * chunks;
+  for (int work = blockIdx.x; work < total; work += gridDim.x) {
+    const int h = work % hkv;
+    if (work != (int)blockIdx.x) it = paged_item_raw(hd, work / hkv);
+    paged_item_check(it, a.max_pages, shift, a.ws, a.err);
+    const int* row = a.table + it.seq * a.table_stride;
+    // element offset of this lane's key of tile t
+    auto locate = [&](int t) -> long long {
+      const int key = it.k0 + t * kFewKeys + lane;
+      if (key >= it.k1) return 0;
+      int id = row[key >> shift];  // key < k1 <= max_pages << shift
+      if ((unsigned)id >= (unsigned)a.c.num_pages) {
+        atomicOr(a.err, kErrBadPage);
+        id = 0;  // (any page: the call has failed)
+      }
+      return id * a.c.page_stride + (((long long)h << shift) + (key & ((1 << shift) - 1))) * dh;
+    };
+    // every lane its row; rows behind the last key are not fetched
+    auto fetch = [&](T* dst, const void* src, int t, long long at, uint32_t bar) {
+      const int nk = min(kFewKeys, it.k1 - it.k0 - t * kFewKeys);
+      if (lane == 0) tc::mbar_expect_tx(bar, nk * row_bytes);
+      __syncwarp();
+      if (lane < nk) copy_row(tc::smem_u32(dst + lane * ld), static_cast<const T*>(src) + at, row_bytes, bar);
+    };
+    const int n_tiles = it.k1 > it.k0 ? (it.k1 - it.k0 + kFewKeys - 1) / kFewKeys : 0;
+    __syncwarp();  // the previous unit's shared memory has been read
+    if (n_tiles > 0) {
+      const long long at = locate(0);
+      fetch(s_k, a.c.k, 0, at, b_k);
+      fetch(s_v, a.c.v, 0, at, b_v);
+    }
+#pragma unroll
+    for (int r = 0; r < RL; ++r) {
+      const int tok = r / group;
+      const T* q = static_cast<const T*>(a.q) + (it.row0 + tok) * a.q_stride + (long long)(h * group + r % group) * dh;
+      for (int c = lane * 4; c < dh; c += 128) {
+        Quad v{0, 0};
+        if (tok < it.n_tok) v = load4(q + c);
+        *reinterpret_cast<ulonglong2*>(s_q + r * dh + c) = make_ulonglong2(v.a, v.b);
+      }
+    }
+    const int lim_min = causal ? min(it.k1, it.pos0 + 1) : it.k1;  // the first token's: no row sees fewer
+    float m[RL], l[RL];
+    Quad o[RL][NCH];
+#pragma unroll
+    for (int r = 0; r < RL; ++r) {
+      m[r] = -INFINITY, l[r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) o[r][c] = Quad{0, 0};
+    }
+    for (int t = 0; t < n_tiles; ++t, ++done) {
+      const int key0 = it.k0 + t * kFewKeys;
+      const bool more = t + 1 < n_tiles;
+      const long long next = more ? locate(t + 1) : 0;
+      __syncwarp();  // (the queries are there)
+      ok = ok && tc::warp_wait(b_k, done & 1, a.err, abort_flag);
+      uint64_t s2[RL];  // sums over even and over odd elements
+#pragma unroll
+      for (int r = 0; r < RL; ++r) s2[r] = 0;
+#pragma unroll (RL == 4 ? 8 : 4)
+      for (int c = 0; c < dh; c += 4) {
+        const Quad k = load4(s_k + lane * ld + c);
+#pragma unroll
+        for (int r = 0; r < RL; ++r) {
+          const Quad q = load4(s_q + r * dh + c);
+          s2[r] = tc::f2_fma(q.b, k.b, tc::f2_fma(q.a, k.a, s2[r]));
+        }
+      }
+      __syncwarp();  // the keys have been read
+      const bool ahead = ok && more;
+      if (ahead) fetch(s_k, a.c.k, t + 1, next, b_k);
+      float s[RL];
+      bool up = false;
+#pragma unroll
+      for (int r = 0; r < RL; ++r) {
+        float even, odd;
+        tc::f2_unpack(s2[r], even, odd);
+        s[r] = (even + odd) * scale_log2;
+      }
+      if (key0 + kFewKeys > lim_min) {
+#pragma unroll
+        for (int r = 0; r < RL; ++r)
+          if (key0 + lane >= (causal ? min(it.k1, it.pos0 + r / group + 1) : it.k1)) s[r] = -INFINITY;
+      }
+#pragma unroll
+      for (int r = 0; r < RL; ++r) up |= s[r] > m[r];
+      if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+        for (int r = 0; r < RL; ++r) {
+          float mx = s[r];
+#pragma unroll
+          for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+          mx = fmaxf(m[r], mx);
+          const float f = m[r] == mx ? 1.f : exp2f(m[r] - mx);
+          m[r] = mx;
+          l[r] *= f;
+          const uint64_t ff = tc::f2_pack(f, f);
+#pragma unroll
+          for (int c = 0; c < NCH; ++c) o[r][c] = Quad{tc::f2_mul(o[r][c].a, ff), tc::f2_mul(o[r][c].b, ff)};
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < RL; r += 4) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = exp2f(s[r + e] - (m[r + e] == -INFINITY ? 0.f : m[r + e]));
+          l[r + e] += p[e];
+        }
+        *reinterpret_cast<float4*>(s_p + lane * PP + r) = make_float4(p[0], p[1], p[2], p[3]);
+      }
+      __syncwarp();  // (the probabilities are there)
+      ok = ok && tc::warp_wait(b_v, done & 1, a.err, abort_flag);
+      const int nk = min(kFewKeys, it.k1 - key0);
+      if (grp < groups) {
+#pragma unroll (RL == 4 ? 8 : 4)
+        for (int kk = grp; kk < nk; kk += groups) {
+          Quad v[NCH];
+#pragma unroll
+          for (int c = 0; c < NCH; ++c) {
+            v[c] = Quad{0, 0};
+            if (c == 0 || chunk + 32 * c < chunks) v[c] = load4(s_v + kk * ld + (chunk + 32 * c) * 4);
+          }
+#pragma unroll
+          for (int r = 0; r < RL; r += 4) {
+            const float4 p = *reinterpret_cast<const float4*>(s_p + kk * PP + r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float w = e == 0 ? p.x : e == 1 ? p.y : e == 2 ? p.z : p.w;
+              const uint64_t ww = tc::f2_pack(w, w);
+#pragma unroll
+              for (int c = 0; c < NCH; ++c)
+                o[r + e][c] = Quad{tc::f2_fma(ww, v[c].a, o[r + e][c].a), tc::f2_fma(ww, v[c].b, o[r + e][c].b)};
+            }
+          }
+        }
+      }
+      __syncwarp();  // the values and the probabilities have been read
+      if (!ok) {
+        // gave up: what is still in flight has to land before the shared memory is given back
+        tc::mbar_drain(b_k, (done + ahead) & 1);
+        tc::mbar_drain(b_v, done & 1);
+        return;
+      }
+      if (more) fetch(s_v, a.c.v, t + 1, next, b_v);
+    }
+    float* part = it.part < 0 ? nullptr : a.ws + ((long long)it.part * hkv + h) * paged_part_floats(16, dh);
+#pragma unroll
+    for (int r = 0; r < RL; ++r) {
+      const int tok = r / group;
+      if (tok >= it.n_tok) break;  // (the same for all lanes)
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+      const bool any = (causal ? min(it.k1, it.pos0 + tok + 1) : it.k1) > it.k0;
+      const float inv = 1.f / l[r];
+      T* dst = static_cast<T*>(a.out) + (it.row0 + tok) * a.out_stride + (long long)(h * group + r % group) * dh;
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        float4 v;
+        tc::f2_unpack(o[r][c].a, v.x, v.y);
+        tc::f2_unpack(o[r][c].b, v.z, v.w);
+        if constexpr (NCH == 1) {  // the groups' sums, in order
+          float4 sum = v;
+          for (int j = 1; j < groups; ++j) {
+            const int from = (lane + j * chunks) & 31;  // (what lanes outside the first group add up is not used)
+            sum.x += __shfl_sync(0xffffffffu, v.x, from), sum.y += __shfl_sync(0xffffffffu, v.y, from);
+            sum.z += __shfl_sync(0xffffffffu, v.z, from), sum.w += __shfl_sync(0xffffffffu, v.w, from);
+          }
+          v = sum;
+        }
+        const int col = (chunk + 32 * c) * 4;
+        if (grp > 0 || col >= dh) continue;
+        if (part) {
+          *reinterpret_cast<float4*>(part + ((long long)(col >> 2) * 16 + r) * 4) = v;
+        } else {
+          v = any ? make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
+          store4(dst + col, v);
+        }
+      }
+      if (part && lane == 0) *reinterpret_cast<float2*>(part + (long long)16 * dh + 2 * r) = make_float2(m[r], l[r]);
+    }
+  }
+}
+
 int log2_of(int x) {
   int s = 0;
   while ((1 << s) < x) ++s;
@@ -531,6 +777,17 @@ cudaError_t simt_launch(const PagedAttnArgs& a, int grid, cudaStream_t st) {
   k_paged_simt<T, R, NC, kOver><<<grid, 256, smem, st>>>(a, log2_of(a.c.page_size), scale_log2);
   return cudaGetLastError();
 }
+// rows the kernel for few rows keeps: what an item can have, rounded up
+int few_rows(int max_q, int g) { return max_q * g <= 4 ? 4 : 8; }
+template <typename T, int RL, int NCH>
+cudaError_t few_launch(const PagedAttnArgs& a, int grid, cudaStream_t st) {
+  static std::atomic<unsigned long long> set;
+  const int smem = few_smem<T>(RL, a.c.dh);
+  if (cudaError_t e = ensure_dynamic_smem(k_paged_few<T, RL, NCH>, few_smem<T>(RL, 128 * NCH), set)) return e;
+  k_paged_few<T, RL, NCH><<<grid, 32, smem, st>>>(a, log2_of(a.c.page_size), 1.4426950408889634f / sqrtf((float)a.c.dh));
+  return cudaGetLastError();
+}
+static_assert(few_smem<float>(8, 256) <= 232448, "exceeds the shared memory one block may have");
 static_assert(simt_smem<float>(64, 256, false) <= 232448, "exceeds the shared memory one block may have");
 
 }  // namespace
@@ -562,6 +819,17 @@ bool paged_plan_shape(int n_seq, int total_q, int max_q, int hq, int hkv, int dh
     return true;
   }
   if (g > 64) return false;
+  if ((long long)max_q * g <= 8) {
+    // (measured beside the kernel.)  Every warp works alone, so even short key ranges are worth cutting.
+    const int rl = few_rows(max_q, g), smem = dtype == 1 ? few_smem<__nv_bfloat16>(rl, dh) : few_smem<float>(rl, dh);
+    const int per_sm = 233472 / (smem + 1024);
+    const float bytes = dtype == 1 ? 2.f : 4.f;
+    s->kind = kPagedFew, s->rows = 16, s->tokens = 16 / g, s->min_piece = 64, s->slots = 148 * (per_sm < 16 ? per_sm : 16);
+    s->piece_unit = 64, s->min_cut = 128;
+    s->ns_key = (2.f + 0.75f * rl) * (8.f + dh / 8.f), s->ns_key_block = 2.f * bytes * dh / 4000.f;
+    s->ns_item = 2500.f, s->ns_part = 200.f, s->ns_join = 2500.f;
+    return true;
+  }
   // 64 rows a block use the FMA units best (16 are bound by shared-memory reads): 256 tokens behind 4096, 16 heads, 298 us
   // against 733.  16 spread a call of few short sequences over the SMs and fill their tiles: 16 documents of 32 tokens, 4 heads
   // of 64, 6.5 us against 9.8, 48 of them 13.2 against 10.1; 8 of 40 tokens, 16 heads, 17.1 against 13.3, 4 of them 12.4
@@ -606,6 +874,14 @@ cudaError_t launch_paged_join(const PagedAttnArgs& a, const PagedPlanShape& s, i
   if (a.c.dtype == 1) return lanes == 8 ? PRISM_JOIN(__nv_bfloat16, 8) : PRISM_JOIN(__nv_bfloat16, 1);
   return lanes == 8 ? PRISM_JOIN(float, 8) : PRISM_JOIN(float, 1);
 #undef PRISM_JOIN
+}
+
+cudaError_t launch_paged_few(const PagedAttnArgs& a, const PagedPlanShape& s, int grid, cudaStream_t st) {
+  const int rl = few_rows(a.max_q, s.group);
+#define PRISM_FEW(T, NCH) (rl == 4 ? few_launch<T, 4, NCH>(a, grid, st) : few_launch<T, 8, NCH>(a, grid, st))
+  if (a.c.dtype == 1) return a.c.dh <= 128 ? PRISM_FEW(__nv_bfloat16, 1) : PRISM_FEW(__nv_bfloat16, 2);
+  return a.c.dh <= 128 ? PRISM_FEW(float, 1) : PRISM_FEW(float, 2);
+#undef PRISM_FEW
 }
 
 cudaError_t launch_paged_simt(const PagedAttnArgs& a, const PagedPlanShape& s, int grid, cudaStream_t st) {

@@ -23,6 +23,7 @@ enum PagedKind : int {
   kPagedTokens = 0,  // up to 32 query rows per sequence and key/value head: warp-level MMA, bound by reading the cache
   kPagedTiles = 1,   // tcgen05, two 128-row tiles per item
   kPagedSimt = 2,    // CUDA cores: fp32, and head sizes without a tensor-core kernel
+  kPagedFew = 3,     // the same for up to 8 query rows per sequence and key/value head: a warp per item and head
 };
 
 struct PagedPlanShape {
@@ -140,6 +141,7 @@ cudaError_t launch_paged_plan(const int* cu, const int* kv_len, int n_seq, int t
 cudaError_t launch_paged_tokens(const PagedAttnArgs& a, const PagedPlanShape& s, int grid_items, cudaStream_t st);
 cudaError_t launch_paged_tiles(const PagedAttnArgs& a, const PagedPlanShape& s, int grid_items, cudaStream_t st);
 cudaError_t launch_paged_simt(const PagedAttnArgs& a, const PagedPlanShape& s, int grid_items, cudaStream_t st);
+cudaError_t launch_paged_few(const PagedAttnArgs& a, const PagedPlanShape& s, int grid_items, cudaStream_t st);
 cudaError_t launch_paged_join(const PagedAttnArgs& a, const PagedPlanShape& s, int max_joins, cudaStream_t st);
 // Uncached tensor map of a bf16 tensor with the 128-byte swizzle; strides in bytes for dimensions 1..rank-1.
 cudaError_t make_tma_nd_bf16(TmaDesc* out, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,

@@ -155,6 +155,7 @@ int prism_op_attention_paged(const void* q, int64_t q_stride, const prism_kv_cac
   const int grid = (int)(!may_cut ? tiles : s.kind == kPagedTiles || all < some ? all : some);
   cudaError_t e = s.kind == kPagedTokens  ? launch_paged_tokens(a, s, grid, S(stream))
                   : s.kind == kPagedTiles ? launch_paged_tiles(a, s, grid, S(stream))
+                  : s.kind == kPagedFew   ? launch_paged_few(a, s, grid, S(stream))
                                           : launch_paged_simt(a, s, grid, S(stream));
   if (e == cudaSuccess && may_cut) e = launch_paged_join(a, s, (int)bound.joins, S(stream));
   return st_of(e);

@@ -452,6 +452,25 @@ def test_attention_on_cuda_cores(P, dtype, impl, hq, hkv, dh, page, new, kv, cau
     Call(P, rng, new, kv, hq, hkv, dh, dtype, causal, page, impl=impl).run()
 
 
+@pytest.mark.parametrize("causal", [1, 0])
+@pytest.mark.parametrize("dtype,hq,hkv,dh,page,new,kv", [
+    (FP32, 4, 4, 128, 16, [1] * 8, [0, 1, 31, 32, 33, 128, 129, 1000]),        # a row that sees nothing; keys around a step
+    (FP32, 8, 2, 64, 32, [1, 2, 0, 2], [64, 65, 9, 5000]),                     # pieces
+    (FP32, 8, 1, 16, 16, [1, 1], [70, 900]),
+    (FP32, 3, 1, 48, 64, [1, 2], [2, 333]),                                    # q_len 2 of 2 keys
+    (FP32, 6, 2, 80, 128, [2, 1], [1, 700]),                                   # q_len 2 of 1 key
+    (FP32, 2, 2, 112, 16, [8, 3, 5], [8, 100, 2000]),
+    (FP32, 4, 2, 144, 256, [1, 4], [300, 257]),
+    (FP32, 8, 1, 256, 32, [1], [3001]),
+    (BF16, 4, 4, 16, 16, [1, 1], [17, 400]),
+    (BF16, 6, 2, 80, 16, [1, 2], [31, 1500]),
+    (BF16, 2, 1, 96, 32, [4, 1], [129, 700]),
+    (BF16, 8, 1, 256, 64, [1, 1], [200, 3000]),
+    (FP32, 8, 8, 64, 16, [1] * 300, list(range(300)))])
+def test_attention_of_single_tokens_on_cuda_cores(P, dtype, hq, hkv, dh, page, new, kv, causal):
+    Call(P, np.random.default_rng(dh + hq), new, kv, hq, hkv, dh, dtype, causal, page).run()
+
+
 @pytest.mark.parametrize("new", [[1, 2, 4], [40, 70, 130]])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_attention_with_scores_far_apart(P, new, dtype):
