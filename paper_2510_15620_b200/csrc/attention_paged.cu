@@ -354,6 +354,8 @@ __global__ void __launch_bounds__(256, R == 16 || kOver ? 2 : 1) k_paged_simt(Pa
   // [2][64] element offset of each key's row, or -1
   long long* s_at = reinterpret_cast<long long*>(reinterpret_cast<unsigned char*>(s_k) + simt_keys<T>(R, dh, kOver));
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  // 16-byte piece `piece0` of row `row0` is this thread's first of a tile, the next one is 256 pieces on (without divisions)
+  const int row0 = tid / pieces, piece0 = tid % pieces, row_step = 256 / pieces, piece_step = 256 % pieces;
   for (int work = blockIdx.x; work < total; work += gridDim.x) {
     const int h = work % hkv;
     if (work != (int)blockIdx.x) it = paged_item_raw(hd, work / hkv);
@@ -375,20 +377,24 @@ __global__ void __launch_bounds__(256, R == 16 || kOver ? 2 : 1) k_paged_simt(Pa
     };
     auto fetch = [&](T* dst, const void* src, int t) {
       const long long* at = s_at + (t & 1) * kKeys;
-      for (int u = tid; u < kKeys * pieces; u += 256) {
-        const int kk = u / pieces, c = (u % pieces) * (16 / (int)sizeof(T));
+      for (int kk = row0, piece = piece0; kk < kKeys;) {
+        const int c = piece * (16 / (int)sizeof(T));
         const long long o = at[kk];
         copy16(dst + kk * ld + c, static_cast<const T*>(src) + (o < 0 ? 0 : o + c), o >= 0);
+        kk += row_step, piece += piece_step;
+        if (piece >= pieces) piece -= pieces, ++kk;
       }
       copies_commit();
     };
     const int n_tiles = it.k1 > it.k0 ? (it.k1 - it.k0 + kKeys - 1) / kKeys : 0;
     __syncthreads();  // the previous item's shared memory has been read
     const T* q = static_cast<const T*>(a.q);
-    for (int u = tid; u < R * pieces; u += 256) {
-      const int r = u / pieces, c = (u % pieces) * (16 / (int)sizeof(T)), tok = r / group;
+    for (int r = row0, piece = piece0; r < R;) {
+      const int c = piece * (16 / (int)sizeof(T)), tok = r / group;
       const bool some = tok < it.n_tok;
-      copy16(s_q + r * ld + c, some ? q + (it.row0 + tok) * a.q_stride + (long long)(h * group + r % group) * dh + c : q, some);
+      copy16(s_q + r * ld + c, some ? q + (it.row0 + tok) * a.q_stride + (long long)(h * group + r - tok * group) * dh + c : q, some);
+      r += row_step, piece += piece_step;
+      if (piece >= pieces) piece -= pieces, ++r;
     }
     locate(0);
     __syncthreads();
