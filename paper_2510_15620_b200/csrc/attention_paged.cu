@@ -284,9 +284,9 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedPlanHeader want, const 
 // different banks.
 // Bound by FMA issue and shared-memory reads at R = 64 (both about 60 % busy), by latency in small calls, by reading the cache
 // at R = 16.
-// Measured, fp32, 16 query and 8 key/value heads of 128: 20 x 352 tokens behind 512 1174 us (33.8 TFLOP/s of causal pairs; single
-// FMAs instead of FMAs on pairs of floats 1566, one block an SM with the probabilities in memory of their own 1372), 1024 tokens
-// behind 8192 2345 us (3026, 2645); 16 documents of 32 tokens, 4 heads of 64, 6.5 us.
+// Measured, fp32, 16 query and 8 key/value heads of 128: 20 x 352 tokens behind 512 1130 us (35 TFLOP/s of causal pairs; single
+// FMAs instead of FMAs on pairs of floats 1566, one block an SM with the probabilities in memory of their own 1372, divisions in
+// the fetches 1174), 1024 tokens behind 8192 2265 us (3026, 2645, 2345); 16 documents of 32 tokens, 4 heads of 64, 6.5 us.
 constexpr int kKeys = 64;
 
 // four neighbouring elements as two pairs of floats, what an FMA on pairs takes
@@ -841,8 +841,12 @@ bool paged_plan_shape(int n_seq, int total_q, int max_q, int hq, int hkv, int dh
   // of 64, 6.5 us against 9.8, 48 of them 13.2 against 10.1; 8 of 40 tokens, 16 heads, 17.1 against 13.3, 4 of them 12.4
   // against 13.2.  (fp32; how deep the cache is, which would decide the cases between, is not known here.)
   const bool small = few || (g <= 16 && (long long)max_q * g <= 96 && ((long long)total_q * g / 64 + n_seq) * hkv < 128);
-  s->kind = kPagedSimt, s->rows = small ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 256, s->slots = 148 * 2;
-  s->ns_key = small ? 10.f : 40.f, s->ns_key_block = 0.f, s->ns_item = 2000.f, s->ns_part = 1000.f, s->ns_join = 2500.f;
+  s->kind = kPagedSimt, s->rows = small ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 128, s->slots = 148 * 2;
+  // Slow keys make cutting worth while earlier: 20 tokens behind 816-1632, 8 / 1 heads of 64, 24 us against 33 with pieces from
+  // 256 keys of tiles from 512 on; 14 sequences of 1-2 tokens behind 435, 28 / 4 heads of 64, 20 against 28.
+  s->piece_unit = kKeys, s->min_cut = busy ? 512 : 128;
+  s->ns_key = small ? 10.f + 0.65f * dh : 25.f + 2.f * dh, s->ns_key_block = 0.f;
+  s->ns_item = 3000.f, s->ns_part = small ? 1000.f : 5000.f, s->ns_join = 2500.f;
   return true;
 }
 
