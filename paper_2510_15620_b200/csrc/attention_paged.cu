@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(256) k_paged_join(PagedPlanHeader want, const 
 // at R = 16.
 // Measured, fp32, 16 query and 8 key/value heads of 128: 20 x 352 tokens behind 512 1130 us (35 TFLOP/s of causal pairs; single
 // FMAs instead of FMAs on pairs of floats 1566, one block an SM with the probabilities in memory of their own 1372, divisions in
-// the fetches 1174), 1024 tokens behind 8192 2265 us (3026, 2645, 2345); 16 documents of 32 tokens, 4 heads of 64, 6.5 us.
+// the fetches 1174), 1024 tokens behind 8192 2265 us (3026, 2645, 2345); 16 documents of 32 tokens, 4 heads of 64, 6.1 us.
 constexpr int kKeys = 64;
 
 // four neighbouring elements as two pairs of floats, what an FMA on pairs takes
@@ -836,10 +836,11 @@ bool paged_plan_shape(int n_seq, int total_q, int max_q, int hq, int hkv, int dh
     s->ns_item = 2500.f, s->ns_part = 200.f, s->ns_join = 2500.f;
     return true;
   }
-  // 64 rows a block use the FMA units best (16 are bound by shared-memory reads): 256 tokens behind 4096, 16 heads, 298 us
-  // against 733.  16 spread a call of few short sequences over the SMs and fill their tiles: 16 documents of 32 tokens, 4 heads
-  // of 64, 6.5 us against 9.8, 48 of them 13.2 against 10.1; 8 of 40 tokens, 16 heads, 17.1 against 13.3, 4 of them 12.4
-  // against 13.2.  (fp32; how deep the cache is, which would decide the cases between, is not known here.)
+  // 64 rows a block use the FMA units best (16 are bound by shared-memory reads): 256 tokens behind 4096, 16 / 8 heads of 128,
+  // 285 us against 707.  16 spread a call of few short sequences over the SMs and fill their tiles: 16 documents of 32 tokens, 4
+  // / 2 heads of 64, 6.1 us against 9.4, 48 of them 12.4 against 9.9; 8 of 40 tokens, 16 / 8 heads of 128, 16.3 against 12.8, 4
+  // of them 11.8 against 12.6.  (fp32.  How deep the cache is, is not known here: 40 tokens behind 4096 take 116 us, 86 with 64
+  // rows.)
   const bool small = few || (g <= 16 && (long long)max_q * g <= 96 && ((long long)total_q * g / 64 + n_seq) * hkv < 128);
   s->kind = kPagedSimt, s->rows = small ? 16 : 64, s->tokens = s->rows / g, s->min_piece = 128, s->slots = 148 * 2;
   // Slow keys make cutting worth while earlier: 20 tokens behind 816-1632, 8 / 1 heads of 64, 24 us against 33 with pieces from
@@ -897,8 +898,8 @@ cudaError_t launch_paged_few(const PagedAttnArgs& a, const PagedPlanShape& s, in
 cudaError_t launch_paged_simt(const PagedAttnArgs& a, const PagedPlanShape& s, int grid, cudaStream_t st) {
   const int dh = a.c.dh;
   // `most`: blocks the lengths may ask for.  Where no SM can get two (or fit two: above head_dim 128), the probabilities keep
-  // memory of their own: 4 x 40 fp32 tokens behind 1000, 8 query and 2 key/value heads of 128, 53 us against 82; 256 tokens
-  // behind 4096, 16 and 8 heads, 376 against 298.
+  // memory of their own: 2 x 100 bf16 tokens behind 300, 8 / 2 heads of 80, 25.5 us against 27.1; 256 fp32 tokens behind 4096,
+  // 16 / 8 heads of 128, 333 against 284.
   const long long keys = (long long)a.max_pages * a.c.page_size;
   const long long pieces = keys > s.min_cut ? (keys + s.min_piece - 1) / s.min_piece : 1;
   const long long most = ((long long)a.total_q / s.tokens + a.n_seq) * a.c.hkv * pieces;
